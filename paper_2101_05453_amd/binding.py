@@ -782,3 +782,266 @@ def sru_prepare(layers, device=0):
     del keep
     _check(rc, "sru_int_prepare")
     return SruModel(h, len(layers), device)
+
+
+# ---------------------------------------------------------------------------
+# include/lm_ops.h: norm into int8 codes, products with 4-bit weights, the gated delta rule
+# ---------------------------------------------------------------------------
+LM_F32, LM_F16, LM_BF16 = 0, 1, 2
+
+
+class RmsNormArgs(C.Structure):
+    """rms_norm_args"""
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("groups", C.c_int32), ("dtype", C.c_int32),
+                ("zero_point", C.c_int32), ("eps", C.c_double), ("scale", C.c_double), ("x_stride", C.c_int64),
+                ("residual_stride", C.c_int64), ("gate_stride", C.c_int64), ("new_residual_stride", C.c_int64)]
+
+
+class W4LinearParams(C.Structure):
+    """w4_linear_params"""
+    _fields_ = [("inputs", C.c_int32), ("outputs", C.c_int32), ("group_size", C.c_int32), ("W", _fp),
+                ("codes", C.POINTER(C.c_int8)), ("scales", _fp), ("bias", _fp)]
+
+
+class W4LinearQuant(C.Structure):
+    """w4_linear_quant"""
+    _fields_ = [("inputs", C.c_int32), ("outputs", C.c_int32), ("group_size", C.c_int32), ("groups", C.c_int32),
+                ("codes", C.POINTER(C.c_int8)), ("scales", _fp)]
+
+
+class DeltaRuleArgs(C.Structure):
+    """delta_rule_args"""
+    _fields_ = [(n, C.c_int32) for n in ("steps", "batch", "key_heads", "value_heads", "key_dim", "value_dim", "dtype",
+                                         "normalize")] + [("scale", C.c_double)] + [
+        (n + "_stride", C.c_int64 * 3) for n in ("q", "k", "v", "y", "g", "beta")]
+
+
+_lm = None  # the library with the entry points below declared, and torch's types by their code
+
+
+def lm_lib():
+    global _lm
+    if _lm is None:
+        import torch
+
+        L = lib()
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        L.rms_norm_forward.restype = C.c_int
+        L.rms_norm_forward.argtypes = [i32, C.POINTER(RmsNormArgs)] + [p] * 9
+        L.w4_linear_prepare.restype = C.c_int
+        L.w4_linear_prepare.argtypes = [C.POINTER(W4LinearParams), i32, C.POINTER(p)]
+        L.w4_linear_get_quant.restype = C.c_int
+        L.w4_linear_get_quant.argtypes = [p, C.POINTER(W4LinearQuant)]
+        L.w4_linear_forward.restype = C.c_int
+        L.w4_linear_forward.argtypes = [p, p, i64, i64, p, C.c_float, i32, p, i64, i32, p]
+        L.w4_linear_destroy.restype = None
+        L.w4_linear_destroy.argtypes = [p]
+        L.delta_rule_workspace_bytes.restype = C.c_size_t
+        L.delta_rule_workspace_bytes.argtypes = [C.POINTER(DeltaRuleArgs)]
+        L.delta_rule_forward.restype = C.c_int
+        L.delta_rule_forward.argtypes = [i32, C.POINTER(DeltaRuleArgs)] + [p] * 10 + [C.c_size_t, p]
+        _lm = L, {torch.float32: LM_F32, torch.float16: LM_F16, torch.bfloat16: LM_BF16}
+    return _lm
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _row_stride(t, like):
+    """Elements between the rows of t, a tensor of like's shape whose leading dimensions collapse into rows; 0 for None."""
+    if t is None:
+        return 0
+    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and t.shape == like.shape
+    if t.is_contiguous():
+        return t.shape[-1]
+    return t.view(-1, t.shape[-1]).stride(0) if t.stride(-1) == 1 else _not_dense()
+
+
+def _not_dense():
+    raise ValueError("the last dimension has to be dense")
+
+
+def _dense(t, shape, dtype, device):
+    assert t.device == device and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()
+    return t
+
+
+def _rms_norm(x, weight, residual, gate, groups, eps, scale, zero_point, codes, scales, y, new_residual):
+    import torch
+
+    L, types = lm_lib()
+    assert x.is_cuda and x.dim() >= 1 and groups >= 1
+    cols = x.shape[-1]
+    _dense(weight, (cols // groups,), torch.float32, x.device)
+    args = RmsNormArgs(x.numel() // cols if cols else 0, cols, groups, types[x.dtype], zero_point, eps, scale or 0.0,
+                       _row_stride(x, x), _row_stride(residual, x), _row_stride(gate, x), _row_stride(new_residual, x))
+    _check(L.rms_norm_forward(x.device.index, args, x.data_ptr(), _ptr(residual), _ptr(gate), weight.data_ptr(), _ptr(codes),
+                              _ptr(scales), _ptr(y), _ptr(new_residual), torch.cuda.current_stream(x.device).cuda_stream),
+           "rms_norm_forward")
+
+
+# rms_norm_forward without codes, on torch device tensors
+def rms_norm(x, weight, residual=None, gate=None, groups=1, eps=1e-6, y=None, new_residual=None):
+    """x: CUDA tensor [..., cols] (float32, float16 or bfloat16; rows may be strided); residual, gate, new_residual: of the
+    same shape and type; weight: float32 [cols / groups].  Returns y, the norm of x + residual in x's type; new_residual,
+    if given, receives x + residual (it may be residual itself).  Asynchronous on torch's current stream."""
+    import torch
+
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else _dense(y, x.shape, x.dtype, x.device)
+    _rms_norm(x, weight, residual, gate, groups, eps, None, 0, None, None, y, new_residual)
+    return y
+
+
+# rms_norm_forward with codes, on torch device tensors
+def rms_norm_quantize(x, weight, residual=None, gate=None, groups=1, eps=1e-6, scale=None, zero_point=0, codes=None,
+                      scales=None, y=None, new_residual=None):
+    """As rms_norm, into int8 codes: returns (codes [..., cols], scales float32 [...]), a scale of each row; or (codes, None)
+    with a fixed scale and zero point, such as a model's (s_x, zp_x).  y, if given, also receives the norm in x's type."""
+    import torch
+
+    assert scale is None or scale > 0
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else _dense(codes, x.shape, torch.int8, x.device)
+    if scale is not None:
+        scales = None
+    elif scales is None:
+        scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    else:
+        _dense(scales, x.shape[:-1], torch.float32, x.device)
+    if y is not None:
+        _dense(y, x.shape, x.dtype, x.device)
+    _rms_norm(x, weight, residual, gate, groups, eps, scale, zero_point, codes, scales, y, new_residual)
+    return codes, scales
+
+
+class W4Linear:
+    """Owns one w4_linear_model."""
+
+    def __init__(self, handle, inputs, outputs, device):
+        self._h = handle
+        self.inputs, self.outputs, self.device = inputs, outputs, device
+
+    def __del__(self):
+        self.destroy()
+
+    # w4_linear_destroy
+    def destroy(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.w4_linear_destroy(self._h)
+        self._h = None
+
+    # w4_linear_get_quant
+    def get_quant(self):
+        q = W4LinearQuant()
+        _check(lm_lib()[0].w4_linear_get_quant(self._h, C.byref(q)), "w4_linear_get_quant")
+        return {"group_size": q.group_size, "codes": _view(q.codes, (q.outputs, q.inputs), np.int8),
+                "scales": _view(q.scales, (q.outputs, q.groups), np.float32)}
+
+    # w4_linear_forward on torch device tensors
+    def forward(self, x, x_scale, zero_point=0, y=None, dtype=None):
+        """x: int8 CUDA tensor [..., inputs] (rows may be strided); x_scale: a number, or float32 [...] with a scale of each
+        row.  Returns y [..., outputs] of `dtype` (default bfloat16), or fills the y given (its rows may be strided).
+        Asynchronous on torch's current stream."""
+        import torch
+
+        L, types = lm_lib()
+        assert x.is_cuda and x.dtype == torch.int8 and x.shape[-1] == self.inputs and x.device.index == self.device
+        shape = x.shape[:-1] + (self.outputs,)
+        if y is None:
+            y = torch.empty(shape, dtype=dtype or torch.bfloat16, device=x.device)
+        else:
+            assert y.device == x.device and y.shape == shape and (dtype is None or y.dtype == dtype)
+        row_scales = None
+        if isinstance(x_scale, torch.Tensor):
+            row_scales, x_scale = _dense(x_scale, x.shape[:-1], torch.float32, x.device).data_ptr(), 1.0
+        _check(L.w4_linear_forward(self._h, x.data_ptr(), _row_stride(x, x), x.numel() // self.inputs, row_scales, x_scale,
+                                   zero_point, y.data_ptr(), _row_stride(y, y), types[y.dtype],
+                                   torch.cuda.current_stream(x.device).cuda_stream), "w4_linear_forward")
+        return y
+
+
+# w4_linear_prepare
+def w4_prepare(W=None, codes=None, scales=None, bias=None, group=128, device=0):
+    """Host arrays: W float32 [N, K], quantized here, or codes int8 [N, K] in -8..7 with scales float32
+    [N, ceil(K / group)]; bias float32 [N] or None.  device = -1 builds a host-only model."""
+    keep = []
+
+    def ptr(a, dtype, shape):
+        if a is None:
+            return None
+        a = np.ascontiguousarray(a, dtype=dtype)
+        assert a.shape == shape, (a.shape, shape)
+        keep.append(a)
+        return a.ctypes.data_as(C.POINTER(C.c_int8 if dtype == np.int8 else C.c_float))
+
+    N, K = (W if W is not None else codes).shape
+    p = W4LinearParams(K, N, group, ptr(W, np.float32, (N, K)), ptr(codes, np.int8, (N, K)),
+                       ptr(scales, np.float32, (N, -(-K // group))), ptr(bias, np.float32, (N,)))
+    h = C.c_void_p()
+    rc = lm_lib()[0].w4_linear_prepare(C.byref(p), device, C.byref(h))
+    del keep
+    _check(rc, "w4_linear_prepare")
+    return W4Linear(h, K, N, device)
+
+
+def _delta_args(q, k, v, y=None, g=None, beta=None, normalize=False, scale=None):
+    L, types = lm_lib()
+    T, B, Hk, Dk = k.shape
+    _, _, Hv, Dv = v.shape
+    assert q.shape == k.shape and v.shape[:2] == k.shape[:2] and q.dtype == k.dtype == v.dtype
+
+    def strides(t):
+        return (0, 0, 0) if t is None else t.stride()[:3]
+
+    return L, DeltaRuleArgs(T, B, Hk, Hv, Dk, Dv, types[q.dtype], int(normalize), Dk ** -0.5 if scale is None else scale,
+                            strides(q), strides(k), strides(v), strides(y), strides(g), strides(beta))
+
+
+# delta_rule_workspace_bytes
+def delta_rule_workspace_bytes(q, k, v):
+    L, args = _delta_args(q, k, v)
+    return L.delta_rule_workspace_bytes(args)
+
+
+def delta_rule_workspace(q, k, v):
+    """A workspace for delta_rule calls of these shapes, for programs that keep it."""
+    import torch
+
+    return torch.empty(max(256, delta_rule_workspace_bytes(q, k, v)), dtype=torch.uint8, device=q.device)
+
+
+# delta_rule_forward on torch device tensors
+def delta_rule(q, k, v, g, beta, state=None, new_state=None, lengths=None, normalize=False, scale=None, y=None, workspace=None):
+    """q, k: CUDA tensors [T, B, Hk, Dk]; v: [T, B, Hv, Dv], all float32, float16 or bfloat16; g (log of the decay), beta:
+    float32 [T, B, Hv]; any strides but a dense last dimension of q, k, v, y.  state: float32 [B, Hv, Dk, Dv], the state
+    before the first step (None: zeros), overwritten with the state after the last one unless new_state takes it.
+    lengths: int32 [B]; outputs behind a row's length stay as they are in y (zeros in a y made here).  scale defaults to
+    Dk ** -0.5.  Returns y [T, B, Hv, Dv].  Asynchronous on torch's current stream."""
+    import torch
+
+    shape, device = v.shape, v.device
+    if y is None:
+        y = (torch.empty if lengths is None else torch.zeros)(shape, dtype=v.dtype, device=device)
+    assert v.is_cuda and q.device == k.device == y.device == g.device == beta.device == device
+    assert y.shape == shape and y.dtype == v.dtype and g.shape == shape[:3] and beta.shape == shape[:3]
+    assert g.dtype == torch.float32 and beta.dtype == torch.float32
+    L, args = _delta_args(q, k, v, y, g, beta, normalize, scale)
+    for t in (q, k, v, y):
+        if t.stride(3) != 1 and t.shape[3] > 1:
+            _not_dense()
+    states = (shape[1], shape[2], k.shape[3], shape[3])
+    if state is not None:
+        _dense(state, states, torch.float32, device)
+    new_state = state if new_state is None else _dense(new_state, states, torch.float32, device)
+    if lengths is not None:
+        _dense(lengths, shape[1:2], torch.int32, device)
+    if workspace is None:
+        need = L.delta_rule_workspace_bytes(args)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    else:
+        assert workspace.device == device and workspace.is_contiguous() and workspace.dtype == torch.uint8
+    _check(L.delta_rule_forward(device.index, args, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
+                                _ptr(lengths), _ptr(state), _ptr(new_state), y.data_ptr(), _ptr(workspace),
+                                workspace.numel() if workspace is not None else 0,
+                                torch.cuda.current_stream(device).cuda_stream), "delta_rule_forward")
+    return y

@@ -1,6 +1,8 @@
 // The gated delta rule (include/lm_ops.h).
 //
 //   S <- e^g S;  u = beta (v - S' k);  S <- S + k u';  y = scale S' q
+#include <algorithm>
+
 #include "lm_common.h"
 
 namespace lstm_int {
@@ -100,15 +102,13 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
     f32x4 u, o;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      // a decay of zero clears the state, whatever it holds
-      const float old = decay == 0.0f ? 0.0f : decay * pk[j], oldq = decay == 0.0f ? 0.0f : decay * pq[j];
-      u[j] = bt * (vf[j] - nk * old);
-      o[j] = nq * (oldq + nk * kq * u[j]);
+      u[j] = bt * (vf[j] - nk * (decay * pk[j]));
+      o[j] = nq * (decay * pq[j] + nk * kq * u[j]);
     }
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) S[i][j] = __builtin_fmaf(nk * kf[i], u[j], decay == 0.0f ? 0.0f : decay * S[i][j]);
+      for (int j = 0; j < 4; ++j) S[i][j] = __builtin_fmaf(nk * kf[i], u[j], decay * S[i][j]);
     if (lane < 4)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -135,6 +135,550 @@ int launch_step(const DeltaArgs &a, hipStream_t s) {
                     : a.Dk <= 128 ? launch(delta_step_kernel<T, 8>, grid, block, s, a) : launch(delta_step_kernel<T, 16>, grid, block, s, a);
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Sequences, kChunk steps at a time.  With c_i the sum of g over the chunk's steps up to i, and S the state before it:
+//   A_ij = beta_i e^(c_i - c_j) k_i'k_j  (j < i),   X = (1 + A)^-1 diag(beta)
+//   u = X (v - diag(e^c) K S),   y = diag(e^c) Q S + P u,   P_ij = e^(c_i - c_j) q_i'k_j  (j <= i)
+//   S <- e^(c_last) S + K' diag(e^(c_last - c)) u
+// X and P do not depend on the state: delta_prep_kernel computes them for all chunks side by side.  delta_scan_kernel
+// carries the state from chunk to chunk.
+//
+// Products: on the bf16 MFMA, whose products are exact and whose sums are float32.  A float32 operand is taken as three
+// bf16 parts that add up to it exactly (8 + 8 + 8 bits of its 24), and of the products of two operands' parts those are
+// left out that are below 2^-24 of the largest: float32 results at three (a bf16 key with the state) to six MFMAs for
+// one, where the float32 MFMA takes 16 times the time.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kChunk = 32;
+constexpr int kMatrix = 2 * 64 * 8;                   // floats of X or P in the workspace: two tiles of 16 rows, 8 floats a lane
+constexpr int kItemFloats = 2 * kMatrix + 4 * kChunk;  // X, P and four factors for each step
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <class T> constexpr int kParts = sizeof(T) == 4 ? 3 : __is_same(T, __bf16) ? 1 : 2;  // bf16 parts of an input
+
+// The MFMA's operand order: lane (i = lane % 16, g = lane / 16) of a 16 x 32 operand has the columns 4 g .. 4 g + 3 and
+// 16 + 4 g .. 16 + 4 g + 3 of row i.  A result (column lane % 16, rows 4 g .. 4 g + 3) of two 16-row tiles then is the
+// other operand of the next product as it lies in the registers.
+union Frag {
+  u32x4 w;
+  bf16x8 b;
+};
+
+__device__ inline f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0); }
+
+__device__ inline uint32_t high_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+__device__ inline float truncated(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
+// x = part 0 + part 1 + part 2, exactly
+__device__ inline void split8(const float *x, Frag out[3]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+    out[0].w[i] = high_halves(a, b);
+    a -= truncated(a);
+    b -= truncated(b);
+    out[1].w[i] = high_halves(a, b);
+    out[2].w[i] = high_halves(a - truncated(a), b - truncated(b));
+  }
+}
+__device__ inline void split8(f32x4 a, f32x4 b, Frag out[3]) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  split8(x, out);
+}
+
+// four neighbouring elements of a row, zeros behind n
+template <class T>
+struct Raw4 {
+  union {
+    uint32_t w[sizeof(T)];
+    T e[4];
+  };
+  __device__ void load(const T *p, int n) {
+    if (n >= 4) {
+      if constexpr (sizeof(T) == 4) {
+        const u32x4 v = *reinterpret_cast<const u32x4_any *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = v[i];
+      } else {
+        const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
+        w[0] = v[0], w[1] = v[1];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = i < n ? p[i] : (T)0.0f;
+    }
+  }
+};
+
+// part p of four values, as two words
+template <int kP>
+__device__ inline void parts4(const float *x, uint32_t out[kP][2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int p = 0; p < kP; ++p) {
+      out[p][i] = high_halves(a, b);
+      a -= truncated(a);
+      b -= truncated(b);
+    }
+  }
+}
+
+// c += a b over the parts of both that matter
+template <int kPa, int kPb>
+__device__ inline f32x4 mfma_parts(const Frag *a, const Frag *b, f32x4 c) {
+#pragma unroll
+  for (int i = kPa - 1; i >= 0; --i)
+#pragma unroll
+    for (int j = kPb - 1; j >= 0; --j)
+      if (i + j <= 2) c = mfma(a[i], b[j], c);
+  return c;
+}
+
+struct ChunkArgs {
+  DeltaArgs d;
+  float *items;  // [B Hv][chunks][kItemFloats]
+  int chunks;
+};
+
+__device__ inline int length_of(const DeltaArgs &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
+
+// One wave per chunk and value head: X, P and the factors of its steps
+//   e^c_i |k_i|^-1,  e^c_i |q_i|^-1 scale,  e^(c_last - c_i) |k_i|^-1,  e^c_last        (norms: 1 without normalize)
+template <class T>
+__global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
+  constexpr int kP = kParts<T>, kLd = 36;
+  const DeltaArgs &d = a.d;
+  __shared__ __attribute__((aligned(16))) float mat[2][kChunk * kLd];  // A, then X; P
+  __shared__ double sum_g[kChunk];
+  __shared__ float rate[kChunk], norm_k[kChunk], norm_q[kChunk];
+  const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
+  const int chunk = blockIdx.x;
+  for (int bh = blockIdx.y; bh < d.B * d.Hv; bh += gridDim.y) {
+    const int b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
+    const int t0 = chunk * kChunk, left = length_of(d, b) - t0;  // steps of the row from here on
+    if (left <= 0) continue;
+    __syncthreads();
+    {
+      const int t = lane & 31;
+      double c = 0;
+      float bt = 0;
+      if (t < left) {
+        const float gv = d.g[b * d.g_stride[1] + h * d.g_stride[2] + (int64_t)(t0 + t) * d.g_stride[0]];
+        c = gv < -1000.0f ? -1000.0 : (double)gv;  // e^-1000 is zero; the sum stays a number
+        bt = d.beta[b * d.beta_stride[1] + h * d.beta_stride[2] + (int64_t)(t0 + t) * d.beta_stride[0]];
+      }
+#pragma unroll
+      for (int m = 1; m < 32; m <<= 1) {
+        union { double v; int w[2]; } x, y;
+        x.v = c;
+        y.w[0] = __shfl_up(x.w[0], m, 32);
+        y.w[1] = __shfl_up(x.w[1], m, 32);
+        if (t >= m) c += y.v;
+      }
+      if (lane < 32) sum_g[t] = c, rate[t] = bt;
+    }
+    const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
+    const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
+    f32x4 kk[3] = {}, qk[3] = {};  // tiles (0,0), (1,0), (1,1)
+    float sk[2] = {0, 0}, sq[2] = {0, 0};
+    for (int kb = 0; kb < d.Dk; kb += 32) {
+      Frag kf[2][kP], qf[2][kP];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const int t = 16 * m + i;
+        const bool in = t < left;
+        const T *kr = kp + (int64_t)(t0 + t) * d.k_stride[0], *qr = qp + (int64_t)(t0 + t) * d.q_stride[0];
+        Raw4<T> rk[2], rq[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = kb + 16 * e + 4 * g;
+          rk[e].load(kr + col, in ? d.Dk - col : 0);
+          rq[e].load(qr + col, in ? d.Dk - col : 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x[4], y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] = (float)rk[e].e[j], y[j] = (float)rq[e].e[j];
+            sk[m] = __builtin_fmaf(x[j], x[j], sk[m]);
+            sq[m] = __builtin_fmaf(y[j], y[j], sq[m]);
+          }
+          uint32_t w[kP][2];
+          parts4<kP>(x, w);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) kf[m][p].w[2 * e] = w[p][0], kf[m][p].w[2 * e + 1] = w[p][1];
+          parts4<kP>(y, w);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) qf[m][p].w[2 * e] = w[p][0], qf[m][p].w[2 * e + 1] = w[p][1];
+        }
+      }
+      kk[0] = mfma_parts<kP, kP>(kf[0], kf[0], kk[0]);
+      kk[1] = mfma_parts<kP, kP>(kf[1], kf[0], kk[1]);
+      kk[2] = mfma_parts<kP, kP>(kf[1], kf[1], kk[2]);
+      qk[0] = mfma_parts<kP, kP>(qf[0], kf[0], qk[0]);
+      qk[1] = mfma_parts<kP, kP>(qf[1], kf[0], qk[1]);
+      qk[2] = mfma_parts<kP, kP>(qf[1], kf[1], qk[2]);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      sk[m] += __shfl_xor(sk[m], 16);
+      sk[m] += __shfl_xor(sk[m], 32);
+      sq[m] += __shfl_xor(sq[m], 16);
+      sq[m] += __shfl_xor(sq[m], 32);
+      if (g == 0) {
+        norm_k[16 * m + i] = d.normalize ? 1.0f / sqrtf(sk[m] + kNormEps) : 1.0f;
+        norm_q[16 * m + i] = (d.normalize ? 1.0f / sqrtf(sq[m] + kNormEps) : 1.0f) * d.scale;
+      }
+    }
+    __syncthreads();
+    float *item = a.items + ((int64_t)bh * a.chunks + chunk) * kItemFloats;
+    if (lane < 32) {
+      float *f = item + 2 * kMatrix;
+      const double c = sum_g[lane], end = sum_g[kChunk - 1];
+      const float e = expf((float)c);
+      f[lane] = e * norm_k[lane];
+      f[kChunk + lane] = e * norm_q[lane];
+      f[2 * kChunk + lane] = expf((float)(end - c)) * norm_k[lane];
+      f[3 * kChunk + lane] = expf((float)end);
+    }
+#pragma unroll
+    for (int tile = 0; tile < 3; ++tile) {
+      const int tj = (tile == 2 ? 16 : 0) + i;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int ti = (tile ? 16 : 0) + 4 * g + r;
+        const float e = ti >= tj ? expf((float)(sum_g[ti] - sum_g[tj])) * norm_k[tj] : 0.0f;
+        mat[0][ti * kLd + tj] = ti > tj ? e * kk[tile][r] * norm_k[ti] * rate[ti] : 0.0f;
+        mat[1][ti * kLd + tj] = ti >= tj ? e * qk[tile][r] * norm_q[ti] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mat[1][(4 * g + r) * kLd + 16 + i] = 0;
+    __syncthreads();
+    // (1 + A)^-1: the 16 x 16 blocks on the diagonal by substitution, a lane a column; then the one below them
+    {
+      const int blk = g & 1;
+      const float *A = mat[0] + 16 * blk * (kLd + 1);
+      float x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float s = r == i ? 1.0f : 0.0f;
+#pragma unroll
+        for (int m = 0; m < r; ++m) s = __builtin_fmaf(-A[r * kLd + m], x[m], s);
+        x[r] = s;
+      }
+      __syncthreads();
+      if (g < 2)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mat[0][(16 * blk + r) * kLd + 16 * blk + i] = x[r];
+    }
+    __syncthreads();
+    {
+      f32x4 m1 = {0, 0, 0, 0}, m2 = {0, 0, 0, 0};
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        m1 = __builtin_amdgcn_mfma_f32_16x16x4f32(mat[0][(16 + i) * kLd + 4 * g + r], mat[0][(4 * g + r) * kLd + i], m1, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        m2 = __builtin_amdgcn_mfma_f32_16x16x4f32(mat[0][(16 + i) * kLd + 16 + 4 * g + r], m1[r], m2, 0, 0, 0);
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        mat[0][(16 + 4 * g + r) * kLd + i] = -m2[r];
+        mat[0][(4 * g + r) * kLd + 16 + i] = 0;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          f32x4 v = *reinterpret_cast<const f32x4 *>(&mat[w][(16 * m + i) * kLd + 16 * e + 4 * g]);
+          if (w == 0) v *= *reinterpret_cast<const f32x4 *>(&rate[16 * e + 4 * g]);
+          *reinterpret_cast<f32x4 *>(item + w * kMatrix + (m * 64 + lane) * 8 + 4 * e) = v;
+        }
+  }
+}
+
+// A workgroup carries kMain * kCols * 16 columns of one head's state through the sequence: kMain waves have 16 kCols columns
+// each, in the registers, for good; four more bring the next chunk's operands into LDS meanwhile, in parts and in the MFMA's
+// order.  kBuffers = 1 where two do not fit.
+template <class T, int kDk, int kMain, int kCols>
+struct Scan {
+  static constexpr int kP = kParts<T>, kBlocks = kDk / 32, kLoad = 4;
+  static constexpr int kThreads = (kMain + kLoad) * 64;
+  struct Buffer {
+    u32x4 k[2][kBlocks][kP][64], q[2][kBlocks][kP][64];  // rows of steps, by key column
+    u32x4 kt[kDk / 16][kP][64];                          // rows of key columns, by step
+    u32x4 x[2][3][64], p[2][3][64];
+    float factor[4][kChunk];
+  };
+  static constexpr int kBuffers = 2 * sizeof(Buffer) <= 160 * 1024 ? 2 : 1;
+};
+
+template <class T, int kDk, int kMain, int kCols>
+__global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs a) {
+  using S = Scan<T, kDk, kMain, kCols>;
+  constexpr int kP = S::kP, kBlocks = S::kBlocks, kBuffers = S::kBuffers;
+  const DeltaArgs &d = a.d;
+  __shared__ typename S::Buffer buffer[kBuffers];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  const int bh = blockIdx.x, b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
+  const int len = length_of(d, b), chunks = (len + kChunk - 1) / kChunk;
+
+  if (wave >= kMain) {
+    // blocks of 4 steps x 4 key columns
+    constexpr int kBlocks4 = 8 * (kDk / 4), kEach = (kBlocks4 + 255) / 256;
+    const int tid = threadIdx.x - kMain * 64;
+    const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
+    const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
+    const float *item = a.items + (int64_t)bh * a.chunks * kItemFloats;
+    Raw4<T> rk[kEach][4], rq[kEach][4];
+    f32x4 rm[2];
+    float rf;
+    auto fetch = [&](int c) {
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        const int id = tid + 256 * n;
+        if (kBlocks4 % 256 && id >= kBlocks4) break;
+        const int step = (id / 64 % 2 * 4 + id % 4) * 4, col = (id / 128 * 16 + id / 4 % 16) * 4;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t t = c * kChunk + step + r;
+          const int there = t < len ? d.Dk - col : 0;
+          rk[n][r].load(kp + t * d.k_stride[0] + col, there);
+          rq[n][r].load(qp + t * d.q_stride[0] + col, there);
+        }
+      }
+      const float *it = item + (int64_t)c * kItemFloats;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) rm[e] = *reinterpret_cast<const f32x4 *>(it + tid * 8 + 4 * e);
+      rf = it[2 * kMatrix + (tid & 127)];
+    };
+    auto put = [&](typename S::Buffer &o) {
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        const int id = tid + 256 * n;
+        if (kBlocks4 % 256 && id >= kBlocks4) break;
+        const int step = (id / 64 % 2 * 4 + id % 4) * 4, col = (id / 128 * 16 + id / 4 % 16) * 4;
+        const int kb = col / 32, kg = col % 16 / 4, kh = col % 32 / 16;
+        auto words = [&](u32x4 &v, int half) { return reinterpret_cast<uint32_t *>(&v) + 2 * half; };
+        uint32_t w[kP][2];
+        float x[4][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int m = step / 16, row = step % 16 + r;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[r][j] = (float)rq[n][r].e[j];
+          parts4<kP>(x[r], w);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) {
+            uint32_t *to = words(o.q[m][kb][p][row + 16 * kg], kh);
+            to[0] = w[p][0], to[1] = w[p][1];
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[r][j] = (float)rk[n][r].e[j];
+          parts4<kP>(x[r], w);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) {
+            uint32_t *to = words(o.k[m][kb][p][row + 16 * kg], kh);
+            to[0] = w[p][0], to[1] = w[p][1];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
+          parts4<kP>(y, w);
+#pragma unroll
+          for (int p = 0; p < kP; ++p) {
+            uint32_t *to = words(o.kt[col / 16][p][col % 16 + j + 16 * (step % 16 / 4)], step / 16);
+            to[0] = w[p][0], to[1] = w[p][1];
+          }
+        }
+      }
+      Frag f[3];
+      split8(rm[0], rm[1], f);
+      u32x4(*to)[3][64] = tid < 128 ? o.x : o.p;
+#pragma unroll
+      for (int p = 0; p < 3; ++p) to[tid / 64 % 2][p][tid & 63] = f[p].w;
+      if (tid < 128) o.factor[tid / 32][tid % 32] = rf;
+    };
+    if (chunks > 0) fetch(0);
+    if constexpr (kBuffers == 2) {
+      if (chunks > 0) put(buffer[0]);
+      if (chunks > 1) fetch(1);
+      __syncthreads();
+      for (int c = 0; c < chunks; ++c) {
+        if (c + 1 < chunks) put(buffer[(c + 1) & 1]);
+        if (c + 2 < chunks) fetch(c + 2);
+        __syncthreads();
+      }
+    } else {
+      for (int c = 0; c < chunks; ++c) {
+        put(buffer[0]);
+        if (c + 1 < chunks) fetch(c + 1);
+        __syncthreads();
+        __syncthreads();
+      }
+    }
+    return;
+  }
+
+  int col[kCols];
+  f32x4 st[kCols][kDk / 16];
+  const int64_t head = ((int64_t)b * d.Hv + h) * d.Dk * d.Dv;
+#pragma unroll
+  for (int n = 0; n < kCols; ++n) {
+    col[n] = ((blockIdx.y * kMain + wave) * kCols + n) * 16 + i;
+#pragma unroll
+    for (int m = 0; m < kDk / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * m + 4 * g + r;
+        st[n][m][r] = d.state && row < d.Dk && col[n] < d.Dv ? d.state[head + (int64_t)row * d.Dv + col[n]] : 0.0f;
+      }
+  }
+  const T *v = static_cast<const T *>(d.v) + b * d.v_stride[1] + h * d.v_stride[2];
+  T *y = static_cast<T *>(d.y) + b * d.y_stride[1] + h * d.y_stride[2];
+  T next[kCols][2][4];
+  auto fetch_v = [&](int c) {
+#pragma unroll
+    for (int n = 0; n < kCols; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t t = c * kChunk + 16 * m + 4 * g + r;
+          next[n][m][r] = t < len && col[n] < d.Dv ? v[t * d.v_stride[0] + col[n]] : (T)0.0f;
+        }
+  };
+  fetch_v(0);
+  if constexpr (kBuffers == 2) __syncthreads();
+  for (int c = 0; c < chunks; ++c) {
+    if constexpr (kBuffers == 1) __syncthreads();
+    const typename S::Buffer &o = buffer[kBuffers == 2 ? c & 1 : 0];
+    f32x4 rhs[kCols][2], out[kCols][2];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) rhs[n][m] = out[n][m] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      Frag s[kCols][3], f[kP];
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) split8(st[n][2 * kb], st[n][2 * kb + 1], s[n]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+#pragma unroll
+        for (int p = 0; p < kP; ++p) f[p].w = o.k[m][kb][p][lane];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) rhs[n][m] = mfma_parts<kP, 3>(f, s[n], rhs[n][m]);
+#pragma unroll
+        for (int p = 0; p < kP; ++p) f[p].w = o.q[m][kb][p][lane];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) out[n][m] = mfma_parts<kP, 3>(f, s[n], out[n][m]);
+      }
+    }
+    Frag part[kCols][3], x[2][3];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const f32x4 fk = *reinterpret_cast<const f32x4 *>(&o.factor[0][16 * m + 4 * g]), fq = *reinterpret_cast<const f32x4 *>(&o.factor[1][16 * m + 4 * g]);
+#pragma unroll
+      for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          rhs[n][m][r] = (float)next[n][m][r] - fk[r] * rhs[n][m][r];
+          out[n][m][r] *= fq[r];
+        }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) x[m][p].w = o.x[m][p][lane];
+    }
+    if (c + 1 < chunks) fetch_v(c + 1);
+    f32x4 u[kCols][2];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      split8(rhs[n][0], rhs[n][1], part[n]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) u[n][m] = mfma_parts<3, 3>(x[m], part[n], f32x4{0, 0, 0, 0});
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int p = 0; p < 3; ++p) x[m][p].w = o.p[m][p][lane];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      split8(u[n][0], u[n][1], part[n]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) out[n][m] = mfma_parts<3, 3>(x[m], part[n], out[n][m]);
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const f32x4 fu = *reinterpret_cast<const f32x4 *>(&o.factor[2][16 * m + 4 * g]);
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) u[n][m] *= fu;
+    }
+    const float whole = o.factor[3][0];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) split8(u[n][0], u[n][1], part[n]);
+#pragma unroll
+    for (int m = 0; m < kDk / 16; ++m) {
+      Frag f[kP];
+#pragma unroll
+      for (int p = 0; p < kP; ++p) f[p].w = o.kt[m][p][lane];
+#pragma unroll
+      for (int n = 0; n < kCols; ++n) st[n][m] = mfma_parts<kP, 3>(f, part[n], st[n][m] * whole);
+    }
+#pragma unroll
+    for (int n = 0; n < kCols; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t t = c * kChunk + 16 * m + 4 * g + r;
+          if (t < len && col[n] < d.Dv) y[t * d.y_stride[0] + col[n]] = (T)out[n][m][r];
+        }
+    __syncthreads();
+  }
+  if (!d.new_state) return;
+#pragma unroll
+  for (int n = 0; n < kCols; ++n)
+#pragma unroll
+    for (int m = 0; m < kDk / 16; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * m + 4 * g + r;
+        if (row < d.Dk && col[n] < d.Dv) d.new_state[head + (int64_t)row * d.Dv + col[n]] = st[n][m][r];
+      }
+}
+
+template <class T, int kDk, int kMain, int kCols>
+int launch_scan(const ChunkArgs &a, hipStream_t s) {
+  const dim3 grid(a.d.B * a.d.Hv, (a.d.Dv + 16 * kMain * kCols - 1) / (16 * kMain * kCols));
+  return launch(delta_scan_kernel<T, kDk, kMain, kCols>, grid, dim3((kMain + 4) * 64), s, a);
+}
+
+template <class T, int kDk>
+int launch_scan(const ChunkArgs &a, hipStream_t s) {
+  const int64_t tiles = (int64_t)a.d.B * a.d.Hv * ((a.d.Dv + 15) / 16);
+  return tiles >= 1024 ? launch_scan<T, kDk, 4, 1>(a, s) : launch_scan<T, kDk, 1, 1>(a, s);
+}
+
+template <class T>
+int launch_chunks(const ChunkArgs &a, hipStream_t s) {
+  const int rc = launch(delta_prep_kernel<T>, dim3(a.chunks, std::min(a.d.B * a.d.Hv, 65535)), dim3(64), s, a);
+  if (rc != LSTM_INT_OK) return rc;
+  return a.d.Dk <= 64 ? launch_scan<T, 64>(a, s) : a.d.Dk <= 128 ? launch_scan<T, 128>(a, s) : launch_scan<T, 256>(a, s);
+}
+
+bool in_chunks(const delta_rule_args *p) { return p->steps >= kChunk; }
+
 int check(const delta_rule_args *p) {
   if (!p || p->steps < 0 || p->batch < 0 || p->key_heads < 1 || p->value_heads < 1 || p->value_heads % p->key_heads || p->key_dim < 1 ||
       p->value_dim < 1 || !lm_type_bytes(p->dtype) || (p->normalize != 0 && p->normalize != 1))
@@ -152,8 +696,8 @@ using namespace lstm_int;
 extern "C" {
 
 size_t delta_rule_workspace_bytes(const delta_rule_args *p) {
-  if (check(p) != LSTM_INT_OK) return 0;
-  return 0;
+  if (check(p) != LSTM_INT_OK || !in_chunks(p)) return 0;
+  return (size_t)p->batch * p->value_heads * ((p->steps + kChunk - 1) / kChunk) * kItemFloats * sizeof(float);
 }
 
 int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, const void *k, const void *v, const float *g,
@@ -177,6 +721,10 @@ int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, 
   const DeviceScope scope(device);
   if (!scope.ok) return LSTM_INT_E_DEVICE;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
+  if (in_chunks(p)) {
+    const ChunkArgs c{a, static_cast<float *>(workspace), (p->steps + kChunk - 1) / kChunk};
+    return p->dtype == LM_F32 ? launch_chunks<float>(c, s) : p->dtype == LM_F16 ? launch_chunks<_Float16>(c, s) : launch_chunks<__bf16>(c, s);
+  }
   return p->dtype == LM_F32 ? launch_step<float>(a, s) : p->dtype == LM_F16 ? launch_step<_Float16>(a, s) : launch_step<__bf16>(a, s);
 }
 

@@ -16,7 +16,7 @@ HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contra
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              "-Wall", "-Wno-unused-function"]
 # in_gemm.hip and the like: MFMA results go to ordinary vector registers, where the requantization reads them without copies
-EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("in_gemm.hip", "deep_gemm.hip", "rec_inst_8.hip", "rec_inst_20.hip", "rec_inst_32.hip", "rec_sparse_inst_8.hip", "rec_sparse_inst_20.hip", "rec_sparse_inst_32.hip", "rec16_inst_4.hip", "rec16_inst_10.hip", "rec16_inst_16.hip", "solo_inst.hip", "row_inst_64.hip", "row_inst_128.hip", "row_inst_192.hip", "row_inst_256.hip", "row_stack_inst_64.hip", "row_stack_inst_128.hip", "row_stack_inst_192.hip", "row_stack_inst_256.hip", "quad_inst_8.hip", "quad_inst_10.hip", "quad_inst_16.hip", "stack_inst_8.hip", "stack_inst_20.hip", "stack_inst_32.hip", "gru_seq.hip", "gru_rows.hip")}
+EXTRA_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("in_gemm.hip", "deep_gemm.hip", "rec_inst_8.hip", "rec_inst_20.hip", "rec_inst_32.hip", "rec_sparse_inst_8.hip", "rec_sparse_inst_20.hip", "rec_sparse_inst_32.hip", "rec16_inst_4.hip", "rec16_inst_10.hip", "rec16_inst_16.hip", "solo_inst.hip", "row_inst_64.hip", "row_inst_128.hip", "row_inst_192.hip", "row_inst_256.hip", "row_stack_inst_64.hip", "row_stack_inst_128.hip", "row_stack_inst_192.hip", "row_stack_inst_256.hip", "quad_inst_8.hip", "quad_inst_10.hip", "quad_inst_16.hip", "stack_inst_8.hip", "stack_inst_20.hip", "stack_inst_32.hip", "gru_seq.hip", "gru_rows.hip", "w4_linear.hip", "delta_rule.hip")}
 # rec_kernel, row_kernel, gru_rows_kernel: what these two passes move out of the step loop, or turn into running pointers of it, ends in spilled registers
 # (eight layers of 2048 cells, 256 rows: 5530 -> 5340 us)
 for _f in ("rec_inst_8.hip", "rec_inst_20.hip", "rec_inst_32.hip", "rec_sparse_inst_8.hip", "rec_sparse_inst_20.hip", "rec_sparse_inst_32.hip", "stack_inst_8.hip", "stack_inst_20.hip", "stack_inst_32.hip", "row_inst_64.hip", "row_inst_128.hip", "row_inst_192.hip", "row_inst_256.hip", "row_stack_inst_64.hip", "row_stack_inst_128.hip", "row_stack_inst_192.hip", "row_stack_inst_256.hip", "gru_rows.hip"):

@@ -44,110 +44,289 @@ struct W4Args {
   float scale;
 };
 
-typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 typedef int64_t i64;
 
-// 16 bytes of a row of x from k on, zeros behind its end
-__device__ inline i32x4 load_x16(const int8_t *row, int k, int K) {
-  if (k + 16 <= K) return (i32x4)*reinterpret_cast<const u32x4_any *>(row + k);
-  union { int8_t b[16]; i32x4 v; } r;
+// n bytes of a row of x from k on, zeros behind its end
+template <class V, int n>
+__device__ inline V load_x(const int8_t *row, int k, int K) {
+  union { int8_t b[n]; V v; } r;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) r.b[i] = k + i < K ? row[k + i] : 0;
-  return r.v;
-}
-__device__ inline i64 load_x8(const int8_t *row, int k, int K) {
-  union { int8_t b[8]; u32x2_any u; i64 v; } r;
-  if (k + 8 <= K) {
-    r.u = *reinterpret_cast<const u32x2_any *>(row + k);
-    return r.v;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r.b[i] = k + i < K ? row[k + i] : 0;
+  for (int i = 0; i < n; ++i) r.b[i] = k + i < K ? row[k + i] : 0;
   return r.v;
 }
 
-// one chunk of 128 inputs for 16 outputs x 16 rows: acc += sum of its groups, scaled
-template <int kGroup>
-__device__ inline void w4_chunk(f32x4 &acc, u32x4 wv, const int8_t *xrow, int k0, int kg, int K, const float *s, const int16_t *sums,
-                                int zp) {
-  constexpr uint32_t kHigh = 0xf0f0f0f0u;
-  const i32x4 hi = (i32x4)(wv & kHigh), lo = (i32x4)((wv << 4) & kHigh);
-  auto begin = [&](int g) {
-    i32x4 c = {0, 0, 0, 0};
-    if (zp) {
-      const int16_t *p = sums + g * kTile;
+constexpr uint32_t kHigh = 0xf0f0f0f0u;
+// A group's sum c, |c| <= 255 * 128 * 128 < 2^22, begins at the bits of the float 1.5 * 2^23: the result's bits then are
+// the float 1.5 * 2^23 + c.
+constexpr float kMagic = 12582912.0f;
+constexpr int kMagicBits = 0x4b400000;
+
+// What the groups of a chunk begin with and are scaled by, for outputs 4 kg .. 4 kg + 3 of a tile
+template <int kGroup, bool kZero>
+struct Scales {
+  static constexpr int kN = kChunk / kGroup;
+  f32x4 s[kN];
+  i32x4 begin[kN];
+  // s, sums: of the chunk's first group
+  __device__ void load(const float *sp, const int16_t *sums, int zp) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) c[r] = -zp * (int)p[r];
+    for (int j = 0; j < kN; ++j) {
+      s[j] = *reinterpret_cast<const f32x4 *>(sp + j * kTile);
+      begin[j] = i32x4{kMagicBits, kMagicBits, kMagicBits, kMagicBits};
+      if constexpr (kZero) {
+        const u32x2_any v = *reinterpret_cast<const u32x2_any *>(sums + j * kTile);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) begin[j][r] = kMagicBits - zp * ((int)(v[r / 2] << (r % 2 ? 0 : 16)) >> 16);
+      }
     }
-    return c;
-  };
-  auto add = [&](i32x4 c, int g) {
-    const f32x4 sv = *reinterpret_cast<const f32x4 *>(s + g * kTile);
+  }
+};
+
+__device__ inline f32x4 add_scaled(i32x4 c, f32x4 s, f32x4 acc) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf((float)c[r], sv[r], acc[r]);
-  };
-  if constexpr (kGroup == 32) {
-    const i64 h[2] = {(i64)((uint32_t)hi[0] | (uint64_t)(uint32_t)hi[1] << 32), (i64)((uint32_t)hi[2] | (uint64_t)(uint32_t)hi[3] << 32)};
-    const i64 l[2] = {(i64)((uint32_t)lo[0] | (uint64_t)(uint32_t)lo[1] << 32), (i64)((uint32_t)lo[2] | (uint64_t)(uint32_t)lo[3] << 32)};
+  for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(__int_as_float(c[r]) - kMagic, s[r], acc[r]);
+  return acc;
+}
+
+// acc += the groups of a chunk, 16 outputs x 16 rows: v the weights as they lie in memory; x the rows' operands of 64
+// inputs each (groups of 32: of 32 each)
+template <int kGroup, bool kZero>
+__device__ inline f32x4 w4_chunk(f32x4 acc, u32x4 v, const i32x4 x[2], const Scales<kGroup, kZero> &sc) {
+  const i32x4 hi = (i32x4)(v & kHigh), lo = (i32x4)((v << 4) & kHigh);
+  if constexpr (kGroup == 64) {
+    acc = add_scaled(__builtin_amdgcn_mfma_i32_16x16x64_i8(hi, x[0], sc.begin[0], 0, 0, 0), sc.s[0], acc);
+    return add_scaled(__builtin_amdgcn_mfma_i32_16x16x64_i8(lo, x[1], sc.begin[1], 0, 0, 0), sc.s[1], acc);
+  } else {
+    const i32x4 c = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi, x[0], sc.begin[0], 0, 0, 0);
+    return add_scaled(__builtin_amdgcn_mfma_i32_16x16x64_i8(lo, x[1], c, 0, 0, 0), sc.s[0], acc);
+  }
+}
+template <bool kZero>
+__device__ inline f32x4 w4_chunk(f32x4 acc, u32x4 v, const i64 x[4], const Scales<32, kZero> &sc) {
+  union { u32x4 v; i64 q[2]; } hi, lo;
+  hi.v = v & kHigh;
+  lo.v = (v << 4) & kHigh;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    acc = add_scaled(__builtin_amdgcn_mfma_i32_16x16x32_i8(j & 1 ? lo.q[j / 2] : hi.q[j / 2], x[j], sc.begin[j], 0, 0, 0), sc.s[j], acc);
+  return acc;
+}
+
+// one row's operands of a chunk, lane kg = lane / 16
+template <int kGroup>
+struct RowOperands {
+  i32x4 x[2];
+  __device__ void load(const int8_t *row, int k0, int kg, int K) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int k = k0 + 64 * j + 16 * kg;
+      x[j] = k0 + kChunk <= K ? (i32x4)*reinterpret_cast<const u32x4_any *>(row + k) : load_x<i32x4, 16>(row, k, K);
+    }
+  }
+};
+template <>
+struct RowOperands<32> {
+  i64 x[4];
+  __device__ void load(const int8_t *row, int k0, int kg, int K) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const i64 xv = load_x8(xrow, k0 + 32 * j + 8 * kg, K);
-      add(__builtin_amdgcn_mfma_i32_16x16x32_i8(j & 1 ? l[j / 2] : h[j / 2], xv, begin(j), 0, 0, 0), j);
+      const int k = k0 + 32 * j + 8 * kg;
+      union { u32x2_any u; i64 v; } r;
+      if (k0 + kChunk <= K) r.u = *reinterpret_cast<const u32x2_any *>(row + k);
+      else r.v = load_x<i64, 8>(row, k, K);
+      x[j] = r.v;
     }
+  }
+};
+
+__device__ inline float row_scale(const W4Args &a, int64_t m) { return a.row_scales ? a.row_scales[m < a.M ? m : a.M - 1] : a.scale; }
+__device__ inline f32x4 bias_of(const W4Args &a, int n) { return a.bias ? *reinterpret_cast<const f32x4 *>(a.bias + n) : f32x4{0, 0, 0, 0}; }
+
+template <class T>
+__device__ inline void w4_store(const W4Args &a, f32x4 acc, float am, f32x4 bias, int64_t m, int n) {
+  T *y = static_cast<T *>(a.y) + m * a.y_stride + n;
+  union {
+    T e[4];
+    uint32_t w[sizeof(T)];
+  } o;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o.e[r] = (T)(am * acc[r] + bias[r]);
+  if (n + 4 <= a.N) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_any *>(y) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
+    else *reinterpret_cast<u32x2_any *>(y) = u32x2_any{o.w[0], o.w[1]};
   } else {
-    const i32x4 x0 = load_x16(xrow, k0 + 16 * kg, K), x1 = load_x16(xrow, k0 + 64 + 16 * kg, K);
-    if constexpr (kGroup == 64) {
-      add(__builtin_amdgcn_mfma_i32_16x16x64_i8(hi, x0, begin(0), 0, 0, 0), 0);
-      add(__builtin_amdgcn_mfma_i32_16x16x64_i8(lo, x1, begin(1), 0, 0, 0), 1);
-    } else {
-      const i32x4 c = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi, x0, begin(0), 0, 0, 0);
-      add(__builtin_amdgcn_mfma_i32_16x16x64_i8(lo, x1, c, 0, 0, 0), 0);
-    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < a.N) y[r] = o.e[r];
   }
 }
 
-template <class T>
-__device__ inline void w4_store(const W4Args &a, f32x4 acc, int64_t m, int n) {
-  const float am = a.row_scales ? a.row_scales[m] : a.scale;
-  T *y = static_cast<T *>(a.y) + m * a.y_stride + n;
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (n + r < a.N) y[r] = (T)(am * acc[r] + (a.bias ? a.bias[n + r] : 0.0f));
-}
-
-// Few rows: a wave has 16 outputs x 16 rows and every split-th chunk of the inputs.
-template <int kGroup, class T>
+// Few rows: a wave has 16 outputs x 16 kRows rows and every split-th chunk of the inputs, kAhead of them requested before
+// the first is used; the parts of a tile meet in LDS, in the order of the waves.
+template <int kGroup, int kRows, bool kZero, class T>
 __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
-  __shared__ f32x4 part[8][64];
+  constexpr int kAhead = kRows == 4 ? 2 : 4, per_chunk = kChunk / kGroup;
+  __shared__ f32x4 part[8][kRows][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tile = blockIdx.x * (8 / a.split) + wave / a.split, p = wave % a.split;
   const int kg = lane >> 4;
-  const int64_t m = (int64_t)blockIdx.y * 16 + (lane & 15);
-  const int8_t *xrow = a.x + (m < a.M ? m : a.M - 1) * a.x_stride;
-  f32x4 acc = {0, 0, 0, 0};
+  const int64_t m0 = (int64_t)blockIdx.y * 16 * kRows + (lane & 15);
+  f32x4 acc[kRows] = {};
   if (tile < a.tiles) {
-    constexpr int per_chunk = kChunk / kGroup;
+    const int8_t *xrow[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) xrow[i] = a.x + (m0 + 16 * i < a.M ? m0 + 16 * i : a.M - 1) * a.x_stride;
     const u32x4 *w = reinterpret_cast<const u32x4 *>(a.w) + (int64_t)tile * a.chunks * 64 + lane;
     const float *s = a.s + (int64_t)tile * a.groups * kTile + 4 * kg;
     const int16_t *sums = a.sums + (int64_t)tile * a.groups * kTile + 4 * kg;
-    for (int c = p; c < a.chunks; c += a.split)
-      w4_chunk<kGroup>(acc, w[c * 64], xrow, c * kChunk, kg, a.K, s + c * per_chunk * kTile, sums + c * per_chunk * kTile, a.zero_point);
+    for (int c0 = p; c0 < a.chunks; c0 += a.split * kAhead) {
+      u32x4 v[kAhead];
+      Scales<kGroup, kZero> sc[kAhead];
+      RowOperands<kGroup> x[kAhead][kRows];
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) {
+        const int c = c0 + n * a.split;
+        if (c >= a.chunks) break;
+        v[n] = __builtin_nontemporal_load(w + (int64_t)c * 64);
+        sc[n].load(s + c * per_chunk * kTile, sums + c * per_chunk * kTile, a.zero_point);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) x[n][i].load(xrow[i], c * kChunk, kg, a.K);
+      }
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) {
+        if (c0 + n * a.split >= a.chunks) break;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) acc[i] = w4_chunk(acc[i], v[n], x[n][i].x, sc[n]);
+      }
+    }
   }
   if (a.split > 1) {
-    part[wave][lane] = acc;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) part[wave][i][lane] = acc[i];
     __syncthreads();
     if (p) return;
-    for (int i = 1; i < a.split; ++i) acc += part[wave + i][lane];
+    for (int j = 1; j < a.split; ++j)
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) acc[i] += part[wave + j][i][lane];
   }
-  if (tile < a.tiles && m < a.M) w4_store<T>(a, acc, m, tile * kTile + 4 * kg);
+  if (tile >= a.tiles) return;
+  const f32x4 bias = bias_of(a, tile * kTile + 4 * kg);
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+    if (m0 + 16 * i < a.M) w4_store<T>(a, acc[i], row_scale(a, m0 + 16 * i), bias, m0 + 16 * i, tile * kTile + 4 * kg);
+}
+
+// Many rows: a workgroup of eight waves has 128 rows x 128 outputs, a wave 64 x 32 of them.  A chunk's operands and scales
+// go through LDS, two chunks deep.  Needs two chunks or more.
+template <int kGroup, bool kZero, class T>
+__global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
+  constexpr int per_chunk = kChunk / kGroup;
+  __shared__ u32x4 xs[2][8][2][64];  // [row tile][64 inputs][operand order]
+  __shared__ u32x4 ws[2][8][64];     // [output tile]
+  __shared__ f32x4 ss[2][8 * per_chunk * 4];
+  __shared__ u32x4 zs[2][8 * per_chunk * 2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, i16 = lane & 15;
+  const int64_t m0 = (int64_t)blockIdx.y * 128;
+  const int nt0 = (wave & 3) * 2, mt0 = (wave >> 2) * 4, tile0 = blockIdx.x * 8 + nt0;
+
+  // a wave brings row tile `wave` and output tile `wave`
+  const int64_t mine = m0 + wave * 16 + i16;
+  const int8_t *xrow = a.x + (mine < a.M ? mine : a.M - 1) * a.x_stride;
+  const u32x4 *w = reinterpret_cast<const u32x4 *>(a.w) + (int64_t)(blockIdx.x * 8 + wave) * a.chunks * 64;
+  // scales and sums: the first threads hold one vector each, the others fetch one of those too (no branch around a load)
+  constexpr int kS = 8 * per_chunk * 4, kZ = 8 * per_chunk * 2;
+  const int st = tid % kS, zt = tid % kZ;
+  const f32x4 *sp = reinterpret_cast<const f32x4 *>(a.s) + ((int64_t)(blockIdx.x * 8 + st / (per_chunk * 4)) * a.groups * 4 + st % (per_chunk * 4));
+  const u32x4 *zp = reinterpret_cast<const u32x4 *>(a.sums) + ((int64_t)(blockIdx.x * 8 + zt / (per_chunk * 2)) * a.groups * 2 + zt % (per_chunk * 2));
+  RowOperands<64> xr;
+  u32x4 wr, zr;
+  f32x4 sr;
+  auto fetch_weights = [&](int c) {
+    wr = (w + (int64_t)c * 64)[(unsigned)lane];
+    sr = sp[c * per_chunk * 4];
+    if constexpr (kZero) zr = zp[c * per_chunk * 2];
+  };
+  auto put = [&](int b) {
+    xs[b][wave][0][lane] = (u32x4)xr.x[0], xs[b][wave][1][lane] = (u32x4)xr.x[1];
+    ws[b][wave][lane] = wr;
+    if (tid < kS) ss[b][tid] = sr;
+    if (kZero && tid < kZ) zs[b][tid] = zr;
+  };
+
+  f32x4 acc[2][4] = {};  // [output tile][row tile]
+  auto compute = [&](int b) {
+    RowOperands<kGroup> x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int8_t *t = reinterpret_cast<const int8_t *>(xs[b][mt0 + i]);
+      if constexpr (kGroup == 32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // 16 bytes of row i16 are those of piece 2 j + kg / 2, of which this lane has one half
+          const int piece = 2 * j + kg / 2;
+          x[i].x[j] = *reinterpret_cast<const i64 *>(t + (piece * 16 + i16) * 16 + kg % 2 * 8);
+        }
+      } else {
+        x[i].x[0] = reinterpret_cast<const i32x4 *>(t)[lane], x[i].x[1] = reinterpret_cast<const i32x4 *>(t)[64 + lane];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      Scales<kGroup, kZero> sc;
+      const int at = (nt0 + j) * per_chunk * kTile + 4 * kg;
+      sc.load(reinterpret_cast<const float *>(ss[b]) + at, reinterpret_cast<const int16_t *>(zs[b]) + at, a.zero_point);
+      const u32x4 v = ws[b][nt0 + j][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = w4_chunk(acc[j][i], v, x[i].x, sc);
+      // keeps the products of the tile behind this one, and their registers, behind it
+      asm volatile("" : "+v"(acc[j][0]), "+v"(acc[j][1]), "+v"(acc[j][2]), "+v"(acc[j][3]));
+    }
+  };
+  // step 0 is the last chunk, which may be short; step n is chunk n - 1, a whole one
+  xr.load(xrow, (a.chunks - 1) * kChunk, kg, a.K);
+  fetch_weights(a.chunks - 1);
+  put(0);
+  __syncthreads();
+  for (int n = 0; n < a.chunks; ++n) {
+    const int next = n + 1 < a.chunks ? n : n - 1;  // behind the end: the last whole chunk again
+#pragma unroll
+    for (int j = 0; j < 2; ++j) xr.x[j] = (i32x4)*reinterpret_cast<const u32x4_any *>(xrow + next * kChunk + 64 * j + 16 * kg);
+    fetch_weights(next);
+    compute(n & 1);
+    put((n + 1) & 1);
+    __syncthreads();
+  }
+  f32x4 bias[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) bias[j] = bias_of(a, (tile0 + j) * kTile + 4 * kg);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t m = m0 + (mt0 + i) * 16 + i16;
+    const float am = row_scale(a, m);
+    if (m >= a.M) continue;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (tile0 + j < a.tiles) w4_store<T>(a, acc[j][i], am, bias[j], m, (tile0 + j) * kTile + 4 * kg);
+  }
+}
+
+template <int kGroup, bool kZero, class T>
+int launch_w4(const W4Args &a, hipStream_t s) {
+  if (a.M > 64 && a.chunks > 1) return launch(w4_block_kernel<kGroup, kZero, T>, dim3((a.tiles + 7) / 8, (a.M + 127) / 128), dim3(512), s, a);
+  const int per_block = 8 / a.split;
+  const dim3 grid((a.tiles + per_block - 1) / per_block, a.M <= 32 ? 1 : (a.M + 63) / 64), block(512);
+  return a.M <= 16   ? launch(w4_rows_kernel<kGroup, 1, kZero, T>, grid, block, s, a)
+         : a.M <= 32 ? launch(w4_rows_kernel<kGroup, 2, kZero, T>, grid, block, s, a)
+                     : launch(w4_rows_kernel<kGroup, 4, kZero, T>, grid, block, s, a);
+}
+
+template <int kGroup, class T>
+int launch_w4(const W4Args &a, hipStream_t s) {
+  return a.zero_point ? launch_w4<kGroup, true, T>(a, s) : launch_w4<kGroup, false, T>(a, s);
 }
 
 template <class T>
-int launch_rows(const W4Args &a, int group, hipStream_t s) {
-  const int per_block = 8 / a.split;
-  const dim3 grid((a.tiles + per_block - 1) / per_block, (a.M + 15) / 16), block(512);
-  return group == 32 ? launch(w4_rows_kernel<32, T>, grid, block, s, a)
-                     : group == 64 ? launch(w4_rows_kernel<64, T>, grid, block, s, a) : launch(w4_rows_kernel<128, T>, grid, block, s, a);
+int launch_w4(const W4Args &a, int group, hipStream_t s) {
+  return group == 32 ? launch_w4<32, T>(a, s) : group == 64 ? launch_w4<64, T>(a, s) : launch_w4<128, T>(a, s);
 }
 
 }  // namespace
@@ -289,12 +468,12 @@ int w4_linear_forward(const w4_linear_model *m, const int8_t *x, int64_t x_strid
   a.M = (int)rows; a.N = m->N; a.K = m->K; a.tiles = (m->N + kTile - 1) / kTile; a.chunks = m->chunks; a.groups = m->dev_groups;
   a.zero_point = zero_point; a.scale = scale;
   a.split = 1;
-  while (a.split < 8 && a.split * 2 <= a.chunks && (int64_t)a.tiles * ((rows + 15) / 16) * a.split < 4096) a.split *= 2;
+  while (a.split < 8 && a.split * 2 <= a.chunks && (int64_t)a.tiles * a.split < 2048) a.split *= 2;
   const DeviceScope scope(m->device);
   if (!scope.ok) return LSTM_INT_E_DEVICE;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  return dtype == LM_F32 ? launch_rows<float>(a, m->group, s)
-                         : dtype == LM_F16 ? launch_rows<_Float16>(a, m->group, s) : launch_rows<__bf16>(a, m->group, s);
+  return dtype == LM_F32 ? launch_w4<float>(a, m->group, s)
+                         : dtype == LM_F16 ? launch_w4<_Float16>(a, m->group, s) : launch_w4<__bf16>(a, m->group, s);
 }
 
 void w4_linear_destroy(w4_linear_model *m) {

@@ -6,6 +6,7 @@ if the library is missing or the call fails, an exception is raised.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -819,6 +820,13 @@ class DeltaRuleArgs(C.Structure):
 _lm = None  # the library with the entry points below declared, and torch's types by their code
 
 
+def _stream(device):
+    """torch's current stream of a device as a hipStream_t: for calls of a few microseconds, without an object for it."""
+    from torch._C import _cuda_getCurrentRawStream
+
+    return _cuda_getCurrentRawStream(device.index)
+
+
 def lm_lib():
     global _lm
     if _lm is None:
@@ -877,7 +885,7 @@ def _rms_norm(x, weight, residual, gate, groups, eps, scale, zero_point, codes, 
     args = RmsNormArgs(x.numel() // cols if cols else 0, cols, groups, types[x.dtype], zero_point, eps, scale or 0.0,
                        _row_stride(x, x), _row_stride(residual, x), _row_stride(gate, x), _row_stride(new_residual, x))
     _check(L.rms_norm_forward(x.device.index, args, x.data_ptr(), _ptr(residual), _ptr(gate), weight.data_ptr(), _ptr(codes),
-                              _ptr(scales), _ptr(y), _ptr(new_residual), torch.cuda.current_stream(x.device).cuda_stream),
+                              _ptr(scales), _ptr(y), _ptr(new_residual), _stream(x.device)),
            "rms_norm_forward")
 
 
@@ -956,7 +964,7 @@ class W4Linear:
             row_scales, x_scale = _dense(x_scale, x.shape[:-1], torch.float32, x.device).data_ptr(), 1.0
         _check(L.w4_linear_forward(self._h, x.data_ptr(), _row_stride(x, x), x.numel() // self.inputs, row_scales, x_scale,
                                    zero_point, y.data_ptr(), _row_stride(y, y), types[y.dtype],
-                                   torch.cuda.current_stream(x.device).cuda_stream), "w4_linear_forward")
+                                   _stream(x.device)), "w4_linear_forward")
         return y
 
 
@@ -984,17 +992,21 @@ def w4_prepare(W=None, codes=None, scales=None, bias=None, group=128, device=0):
     return W4Linear(h, K, N, device)
 
 
+_delta_layout = struct.Struct("@8id18q")
+
+
 def _delta_args(q, k, v, y=None, g=None, beta=None, normalize=False, scale=None):
     L, types = lm_lib()
     T, B, Hk, Dk = k.shape
     _, _, Hv, Dv = v.shape
     assert q.shape == k.shape and v.shape[:2] == k.shape[:2] and q.dtype == k.dtype == v.dtype
 
-    def strides(t):
-        return (0, 0, 0) if t is None else t.stride()[:3]
-
-    return L, DeltaRuleArgs(T, B, Hk, Hv, Dk, Dv, types[q.dtype], int(normalize), Dk ** -0.5 if scale is None else scale,
-                            strides(q), strides(k), strides(v), strides(y), strides(g), strides(beta))
+    none = (0, 0, 0)
+    # the struct from its bytes: a step's call is short, and eighteen strides set one by one are a third of it
+    return L, DeltaRuleArgs.from_buffer_copy(_delta_layout.pack(
+        T, B, Hk, Hv, Dk, Dv, types[q.dtype], int(normalize), Dk ** -0.5 if scale is None else scale, *q.stride()[:3],
+        *k.stride()[:3], *v.stride()[:3], *(none if y is None else y.stride()[:3]), *(none if g is None else g.stride()[:3]),
+        *(none if beta is None else beta.stride()[:3])))
 
 
 # delta_rule_workspace_bytes
@@ -1043,5 +1055,5 @@ def delta_rule(q, k, v, g, beta, state=None, new_state=None, lengths=None, norma
     _check(L.delta_rule_forward(device.index, args, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
                                 _ptr(lengths), _ptr(state), _ptr(new_state), y.data_ptr(), _ptr(workspace),
                                 workspace.numel() if workspace is not None else 0,
-                                torch.cuda.current_stream(device).cuda_stream), "delta_rule_forward")
+                                _stream(device)), "delta_rule_forward")
     return y

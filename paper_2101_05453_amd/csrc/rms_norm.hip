@@ -3,8 +3,10 @@
 //   r = x + residual;  n = r / sqrt(mean(r^2) + eps) * weight [* gate * sigma(gate)];  codes = floor(n / s + 1/2)
 //
 // One pass over memory: a row stays in the registers of one, four or sixteen waves, eight neighbouring columns ("a chunk")
-// per lane and slot, as it lies in memory, from its load to the store of its codes.  What is summed and compared is double
-// precision: the products are then exact enough that a code at the border between two is the one of the definition.
+// per lane and slot, as it lies in memory, from its load to the store of its codes.  A code at the border between two has
+// to be the definition's, so sums of squares are double precision and n is evaluated twice: in float32 for every element,
+// and in double precision for the few that this leaves open -- the row's largest, which the scale is made of, and those
+// whose n / s comes out within 2^-12 of a border.
 #include "lm_common.h"
 
 namespace lstm_int {
@@ -14,7 +16,7 @@ namespace {
 // largest is 127, say); n / s is right to 2^-45, and what is half way goes up.
 constexpr double kHalf = 0.5 + 0x1p-40;
 
-constexpr int kSlots = 4;  // chunks per lane: 2048 columns per wave
+constexpr int kMostSlots = 4;  // chunks per lane: 2048 columns per wave
 
 struct NormArgs {
   const void *x, *residual, *gate;
@@ -24,7 +26,8 @@ struct NormArgs {
   void *y, *new_residual;
   int64_t x_stride, residual_stride, gate_stride, new_residual_stride;
   int rows, cols, groups, D;
-  int lanes, per_group;  // groups > 1: a group takes `lanes` (a power of two) lanes and per_group slots of them
+  int lanes, per_group;  // a group takes `lanes` (a power of two) lanes and per_group slots of them
+  int row_lanes;         // lanes of a wave that a row takes: 64, or `lanes` where a wave has several rows
   int slots;
   int zero_point;
   double eps, scale, inv_d;
@@ -38,71 +41,67 @@ __device__ inline double shfl_xor_d(double v, int mask) {
   return b.d;
 }
 
-template <class T, int kWaves, bool kGate>
+template <class T, int kWaves, int kSlots, bool kGate>
 __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(NormArgs a) {
   constexpr int kBlockWaves = kWaves == 16 ? 16 : 4;
-  __shared__ double part[2][kBlockWaves];
+  __shared__ double part[3][kBlockWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % kWaves;
-  const int64_t row_at = (int64_t)blockIdx.x * (kBlockWaves / kWaves) + wave / kWaves;
-  const bool live = row_at < a.rows;
-  const int64_t row = live ? row_at : a.rows - 1;  // waves behind the last row follow it and store nothing
   const bool whole = a.groups == 1;
+  const int row_lane = lane & (a.row_lanes - 1);
+  const int64_t row_at = ((int64_t)blockIdx.x * (kBlockWaves / kWaves) + wave / kWaves) * (64 / a.row_lanes) + lane / a.row_lanes;
+  const bool live = row_at < a.rows;
+  const int64_t row = live ? row_at : a.rows - 1;  // lanes behind the last row follow it and store nothing
 
-  int col[kSlots], count[kSlots], first[kSlots];  // first: the chunk's column within its group
-  bool last[kSlots];                              // the last slot of a group
-  {
-    int it = 0, c = 0;
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      int group, chunk;
-      if (whole) {
-        group = 0;
-        chunk = (s * kWaves + w) * 64 + lane;
-        last[s] = s == kSlots - 1;
-      } else {
-        group = (it * kWaves + w) * (64 / a.lanes) + lane / a.lanes;
-        chunk = c * a.lanes + lane % a.lanes;
-        last[s] = c == a.per_group - 1;
-        if (++c == a.per_group) c = 0, ++it;
-      }
-      first[s] = chunk * 8;
-      col[s] = group * a.D + chunk * 8;
-      count[s] = s < a.slots && group < a.groups ? max(0, min(8, a.D - chunk * 8)) : 0;
+  // a slot's chunk: its column, its column within the group, the columns it has
+  struct Place {
+    int col, first, count;
+  };
+  auto place = [&](int s) {
+    int group = 0, chunk;
+    if (whole) {
+      chunk = (s * kWaves + w) * a.row_lanes + row_lane;
+    } else {
+      group = (s / a.per_group * kWaves + w) * (64 / a.lanes) + lane / a.lanes;
+      chunk = s % a.per_group * a.lanes + lane % a.lanes;
     }
-  }
+    return Place{group * a.D + chunk * 8, chunk * 8, s < a.slots && group < a.groups ? max(0, min(8, a.D - chunk * 8)) : 0};
+  };
+  Place at[kSlots];
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s) at[s] = place(s);
 
   const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
   const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
+  const T *gate = kGate ? static_cast<const T *>(a.gate) + row * a.gate_stride : nullptr;
   Raw8<T> rx[kSlots], rr[kSlots], rg[kGate ? kSlots : 1];
 #pragma unroll
   for (int s = 0; s < kSlots; ++s) {
-    if (count[s] > 0) rx[s].load(x + col[s], count[s]);
-    if (count[s] > 0 && res) rr[s].load(res + col[s], count[s]);
-    if constexpr (kGate)
-      if (count[s] > 0) rg[s].load(static_cast<const T *>(a.gate) + row * a.gate_stride + col[s], count[s]);
+    if (at[s].count <= 0) continue;
+    rx[s].load(x + at[s].col, at[s].count);
+    if (res) rr[s].load(res + at[s].col, at[s].count);
+    if constexpr (kGate) rg[s].load(gate + at[s].col, at[s].count);
   }
 
-  double n[kSlots][8], inv[kSlots], sum = 0;
+  double inv[kSlots], sum = 0;
 #pragma unroll
   for (int s = 0; s < kSlots; ++s) {
-    if (count[s] > 0) {
+    if (at[s].count > 0) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {  // elements behind the end are zeros
         double r = (double)(float)rx[s].e[i];
         if (res) r += (double)(float)rr[s].e[i];
-        n[s][i] = r;
         sum = __builtin_fma(r, r, sum);
       }
     }
     inv[s] = 0;
-    if (!whole && last[s]) {
+    if (!whole && s % a.per_group == a.per_group - 1) {
       for (int m = a.lanes >> 1; m > 0; m >>= 1) sum += shfl_xor_d(sum, m);
       inv[s] = 1.0 / sqrt(sum * a.inv_d + a.eps);
       sum = 0;
     }
   }
   if (whole) {
-    for (int m = 32; m > 0; m >>= 1) sum += shfl_xor_d(sum, m);
+    for (int m = a.row_lanes >> 1; m > 0; m >>= 1) sum += shfl_xor_d(sum, m);
     if constexpr (kWaves > 1) {
       if (lane == 0) part[0][wave] = sum;
       __syncthreads();
@@ -116,100 +115,186 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
   } else {
 #pragma unroll
     for (int s = kSlots - 2; s >= 0; --s)
-      if (!last[s]) inv[s] = inv[s + 1];
+      if (s % a.per_group != a.per_group - 1) inv[s] = inv[s + 1];
+  }
+  auto inv_of = [&](int s) {  // s known at run time only
+    double v = inv[0];
+#pragma unroll
+    for (int k = 1; k < kSlots; ++k)
+      if (s == k) v = inv[k];
+    return v;
+  };
+  // n in double precision, of memory again: for single elements, and one copy of the code for all of them
+  auto n64 = [&](const Place &p, double iv, int i) {
+    double v = (double)(float)x[p.col + i];
+    if (res) v += (double)(float)res[p.col + i];
+    v = v * iv * (double)a.weight[p.first + i];
+    if constexpr (kGate) {
+      const double z = (double)(float)gate[p.col + i];
+      v *= z / (1.0 + exp(-z));
+    }
+    return v;
+  };
+
+  if (a.y) {
+    T *y = static_cast<T *>(a.y) + row * a.cols;
+#pragma unroll 1
+    for (int s = 0; s < a.slots; ++s) {
+      const Place p = place(s);
+      const double iv = inv_of(s);
+      if (live)
+#pragma unroll 1
+        for (int i = 0; i < p.count; ++i) y[p.col + i] = (T)(float)n64(p, iv, i);
+    }
   }
 
+  if (a.codes) {
+    // n in float32, some ten roundings off
+    float n[kSlots][8], top = 0;
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      if (at[s].count <= 0) continue;
+      const float iv = (float)inv[s];
+      Raw8<float> wt;
+      wt.load(a.weight + at[s].first, at[s].count);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float v = (float)rx[s].e[i];
+        if (res) v += (float)rr[s].e[i];
+        v = v * iv * wt.e[i];
+        if constexpr (kGate) {
+          const float z = (float)rg[s].e[i];
+          v *= z * __builtin_amdgcn_rcpf(1.0f + expf(-z));
+        }
+        n[s][i] = v;
+        // a NaN or a number that float32 may not hold to all its bits: the whole row in double precision
+        const float m = fabsf(v);
+        top = fmaxf(top, m <= 0x1p80f ? m : __builtin_inff());
+      }
+    }
+
+    constexpr float kNear = 0x1p-12f;
+    static_assert(kSlots * 8 <= 32, "a bit for each element of a lane");
+    int8_t *codes = a.codes + row * a.cols;
+    auto store = [&](const Place &p, const int8_t q[8]) {
+      if (!live) return;
+      if (p.count == 8) {
+        union { int8_t b[8]; u32x2_any v; } o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o.b[i] = q[i];
+        *reinterpret_cast<u32x2_any *>(codes + p.col) = o.v;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < p.count) codes[p.col + i] = q[i];
+      }
+    };
+    uint32_t open = 0;  // elements whose code float32 does not decide
+    if (a.scale != 0) {
+      const float mul = (float)(1.0 / a.scale);
+      const bool usable = mul >= 0x1p-80f && mul <= 0x1p80f;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        if (at[s].count <= 0) continue;
+        int8_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float m = fabsf(n[s][i]), v = n[s][i] * mul + 0.5f, f = floorf(v);
+          // beyond 512 the code is at an end whatever v is; a product below float32's normal range is next to no border
+          const bool sure = usable && m <= 0x1p80f && (m >= 0x1p-80f || m == 0) && (fabsf(v) > 512.0f || (v - f > kNear && v - f < 1 - kNear));
+          if (!sure && i < at[s].count) open |= 1u << (8 * s + i);
+          q[i] = (int8_t)min(max((int)fminf(fmaxf(f, -512.0f), 512.0f) + a.zero_point, -128), 127);
+        }
+        store(at[s], q);
+      }
+#pragma unroll 1
+      for (; open; open &= open - 1) {
+        const int k = __builtin_ctz(open);
+        const Place p = place(k / 8);
+        const double e = floor(n64(p, inv_of(k / 8), k % 8) / a.scale + 0.5) + a.zero_point;
+        if (live) codes[p.col + k % 8] = (int8_t)(e != e ? 0 : (int)fmin(fmax(e, -128.0), 127.0));
+      }
+    } else {
+      for (int m = a.row_lanes >> 1; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+      if constexpr (kWaves > 1) {
+        if (lane == 0) part[1][wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, (float)part[1][wave - w + i]);
+      }
+      const bool in_float = top >= 0x1p-80f && top <= 0x1p80f;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < at[s].count && !(in_float && fabsf(n[s][i]) < top * (1 - 0x1p-18f))) open |= 1u << (8 * s + i);
+      double most = 0;
+#pragma unroll 1
+      for (; open; open &= open - 1) {
+        const int k = __builtin_ctz(open);
+        const double v = fabs(n64(place(k / 8), inv_of(k / 8), k % 8));
+        most = fmax(most, v <= 0x1p1020 ? v : __builtin_inf());
+      }
+      for (int m = a.row_lanes >> 1; m > 0; m >>= 1) most = fmax(most, shfl_xor_d(most, m));
+      if constexpr (kWaves > 1) {
+        if (lane == 0) part[2][wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) most = fmax(most, part[2][wave - w + i]);
+      }
+      const bool bad = !__builtin_isfinite(most);
+      const double mul = most > 0 && !bad ? 127.0 / most : 0.0;
+      if (live && row_lane == 0 && w == 0) a.scales[row] = bad ? __builtin_nanf("") : (float)(most / 127.0);
+      const float mul32 = (float)mul;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        if (at[s].count <= 0) continue;
+        int8_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = bad ? 0.0f : n[s][i] * mul32 + 0.5f, f = floorf(v);
+          if (!bad && i < at[s].count && !(in_float && v - f > kNear && v - f < 1 - kNear)) open |= 1u << (8 * s + i);
+          q[i] = (int8_t)(int)fminf(fmaxf(f, -127.0f), 127.0f);
+        }
+        store(at[s], q);
+      }
+#pragma unroll 1
+      for (; open; open &= open - 1) {
+        const int k = __builtin_ctz(open);
+        const Place p = place(k / 8);
+        const double e = floor(n64(p, inv_of(k / 8), k % 8) * mul + kHalf);
+        if (live) codes[p.col + k % 8] = (int8_t)(int)e;
+      }
+    }
+  }
+
+  // last: it may be in the place of x or of the residual
   if (live && a.new_residual) {
     T *out = static_cast<T *>(a.new_residual) + row * a.new_residual_stride;
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-      if (count[s] > 0) {
-        Raw8<T> o;
+    for (int s = 0; s < kSlots; ++s) {
+      if (at[s].count <= 0) continue;
+      Raw8<T> o;
+      // the float32 sum: of two 16-bit numbers it is exact wherever the next rounding could see a difference
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o.e[i] = (T)(float)n[s][i];
-        o.store(out + col[s], count[s]);
-      }
-  }
-
-  double most = 0;
-  bool bad = false;
-#pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    if (count[s] <= 0) continue;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i >= count[s]) continue;
-      double v = n[s][i] * inv[s] * (double)a.weight[first[s] + i];
-      if constexpr (kGate) {
-        const double z = (double)(float)rg[s].e[i];
-        v *= z / (1.0 + exp(-z));
-      }
-      n[s][i] = v;
-      bad |= !__builtin_isfinite(v);
-      most = fmax(most, fabs(v));
-    }
-  }
-
-  if (live && a.y) {
-    T *y = static_cast<T *>(a.y) + row * a.cols;
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-      if (count[s] > 0) {
-        Raw8<T> o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o.e[i] = (T)(float)n[s][i];
-        o.store(y + col[s], count[s]);
-      }
-  }
-  if (!a.codes) return;
-
-  double mul = 0, div = a.scale;
-  if (a.scale == 0) {
-    if (bad) most = __builtin_inf();
-    for (int m = 32; m > 0; m >>= 1) most = fmax(most, shfl_xor_d(most, m));
-    if constexpr (kWaves > 1) {
-      if (lane == 0) part[1][wave] = most;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) most = fmax(most, part[1][wave - w + i]);
-    }
-    bad = !__builtin_isfinite(most);
-    mul = most > 0 && !bad ? 127.0 / most : 0.0;
-    if (live && lane == 0 && w == 0) a.scales[row] = bad ? __builtin_nanf("") : (float)(most / 127.0);
-  }
-  if (!live) return;
-  int8_t *codes = a.codes + row * a.cols;
-#pragma unroll
-  for (int s = 0; s < kSlots; ++s) {
-    if (count[s] <= 0) continue;
-    union { int8_t q[8]; u32x2_any v; } o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      double v;
-      if (a.scale == 0) {
-        v = bad ? 0.0 : floor(n[s][i] * mul + kHalf);
-      } else {
-        v = floor(n[s][i] / div + 0.5) + a.zero_point;
-        v = v != v ? 0.0 : fmin(fmax(v, -128.0), 127.0);
-      }
-      o.q[i] = (int8_t)(int)v;
-    }
-    if (count[s] == 8) {
-      *reinterpret_cast<u32x2_any *>(codes + col[s]) = o.v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < count[s]) codes[col[s] + i] = o.q[i];
+      for (int i = 0; i < 8; ++i) o.e[i] = (T)((float)rx[s].e[i] + (float)rr[s].e[i]);
+      o.store(out + at[s].col, at[s].count);
     }
   }
 }
 
+template <class T, int kWaves, int kSlots>
+int launch_norm(const NormArgs &a, hipStream_t s) {
+  constexpr int threads = kWaves == 16 ? 1024 : 256;
+  const int per_block = threads / 64 / kWaves * (64 / a.row_lanes);
+  const dim3 grid((a.rows + per_block - 1) / per_block);
+  return a.gate ? launch(rms_norm_kernel<T, kWaves, kSlots, true>, grid, dim3(threads), s, a)
+                : launch(rms_norm_kernel<T, kWaves, kSlots, false>, grid, dim3(threads), s, a);
+}
+
 template <class T, int kWaves>
 int launch_norm(const NormArgs &a, hipStream_t s) {
-  constexpr int threads = kWaves == 16 ? 1024 : 256, per_block = threads / 64 / kWaves;
-  const dim3 grid((a.rows + per_block - 1) / per_block);
-  return a.gate ? launch(rms_norm_kernel<T, kWaves, true>, grid, dim3(threads), s, a)
-                : launch(rms_norm_kernel<T, kWaves, false>, grid, dim3(threads), s, a);
+  return a.slots == 1 ? launch_norm<T, kWaves, 1>(a, s) : a.slots == 2 ? launch_norm<T, kWaves, 2>(a, s) : launch_norm<T, kWaves, kMostSlots>(a, s);
 }
 
 template <class T>
@@ -256,11 +341,12 @@ extern "C" int rms_norm_forward(int32_t device, const rms_norm_args *p, const vo
   while (a.lanes < 64 && a.lanes < chunks) a.lanes *= 2;
   a.per_group = (chunks + a.lanes - 1) / a.lanes;
   int waves = 1;
-  while (waves < 16 && slots_of(a, waves) > kSlots) waves *= 4;
+  while (waves < 16 && slots_of(a, waves) > kMostSlots) waves *= 4;
   // few rows: more waves for each, as long as they shorten it
   while (waves < 16 && a.rows * (int64_t)waves < 1024 && slots_of(a, waves) > 1) waves *= 4;
   a.slots = slots_of(a, waves);
-  if (a.slots > kSlots) return LSTM_INT_E_UNSUPPORTED;
+  a.row_lanes = a.groups == 1 && waves == 1 && a.slots == 1 ? a.lanes : 64;  // short rows: several to a wave
+  if (a.slots > kMostSlots) return LSTM_INT_E_UNSUPPORTED;
 
   const DeviceScope scope(device);
   if (!scope.ok) return LSTM_INT_E_DEVICE;

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
       if (s == k) v = inv[k];
     return v;
   };
-  // n in double precision, of memory again: for single elements, and one copy of the code for all of them
+  // n in double precision, of memory again: for single elements, by their number
   auto n64 = [&](const Place &p, double iv, int i) {
     double v = (double)(float)x[p.col + i];
     if (res) v += (double)(float)res[p.col + i];
@@ -138,19 +138,31 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
 
   if (a.y) {
     T *y = static_cast<T *>(a.y) + row * a.cols;
-#pragma unroll 1
-    for (int s = 0; s < a.slots; ++s) {
-      const Place p = place(s);
-      const double iv = inv_of(s);
-      if (live)
-#pragma unroll 1
-        for (int i = 0; i < p.count; ++i) y[p.col + i] = (T)(float)n64(p, iv, i);
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      if (at[s].count <= 0) continue;
+      Raw8<float> wt;
+      Raw8<T> o;
+      wt.load(a.weight + at[s].first, at[s].count);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        double v = (double)(float)rx[s].e[i];
+        if (res) v += (double)(float)rr[s].e[i];
+        v = v * inv[s] * (double)wt.e[i];
+        if constexpr (kGate) {
+          const double z = (double)(float)rg[s].e[i];
+          v *= z / (1.0 + exp(-z));
+        }
+        o.e[i] = (T)(float)v;
+      }
+      if (live) o.store(y + at[s].col, at[s].count);
     }
   }
 
   if (a.codes) {
-    // n in float32, some ten roundings off
-    float n[kSlots][8], top = 0;
+    // n in float32, at most ten roundings off
+    float n[kSlots][8];
+    uint32_t largest = 0;  // bits of the largest |n|; of a NaN, if there is one
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       if (at[s].count <= 0) continue;
@@ -164,16 +176,19 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
         v = v * iv * wt.e[i];
         if constexpr (kGate) {
           const float z = (float)rg[s].e[i];
-          v *= z * __builtin_amdgcn_rcpf(1.0f + expf(-z));
+          // e^-z = 2^(t + lo), t the rounded product
+          constexpr float kLog2e = -1.44269504f, kLow = -1.92596299e-8f, kLn2 = 0.693147181f;
+          const float t = z * kLog2e, lo = __builtin_fmaf(z, kLow, __builtin_fmaf(z, kLog2e, -t));
+          const float e = __builtin_amdgcn_exp2f(t);
+          v *= z * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, fabsf(t) < 128.0f ? lo * kLn2 : 0.0f, e));
         }
         n[s][i] = v;
-        // a NaN or a number that float32 may not hold to all its bits: the whole row in double precision
-        const float m = fabsf(v);
-        top = fmaxf(top, m <= 0x1p80f ? m : __builtin_inff());
+        largest = max(largest, __float_as_uint(v) & 0x7fffffffu);
       }
     }
 
-    constexpr float kNear = 0x1p-12f;
+    // v = n / s + 1/2 decides its floor where it is further from a border than ten roundings of it
+    auto decided = [](float v) { return fabsf(v - floorf(v) - 0.5f) < __builtin_fmaf(fabsf(v), -0x1p-20f, 0.5f - 0x1p-20f); };
     static_assert(kSlots * 8 <= 32, "a bit for each element of a lane");
     int8_t *codes = a.codes + row * a.cols;
     auto store = [&](const Place &p, const int8_t q[8]) {
@@ -201,7 +216,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
         for (int i = 0; i < 8; ++i) {
           const float m = fabsf(n[s][i]), v = n[s][i] * mul + 0.5f, f = floorf(v);
           // beyond 512 the code is at an end whatever v is; a product below float32's normal range is next to no border
-          const bool sure = usable && m <= 0x1p80f && (m >= 0x1p-80f || m == 0) && (fabsf(v) > 512.0f || (v - f > kNear && v - f < 1 - kNear));
+          const bool sure = usable && m <= 0x1p80f && (m >= 0x1p-80f || m == 0) && (fabsf(v) > 512.0f || decided(v));
           if (!sure && i < at[s].count) open |= 1u << (8 * s + i);
           q[i] = (int8_t)min(max((int)fminf(fmaxf(f, -512.0f), 512.0f) + a.zero_point, -128), 127);
         }
@@ -215,19 +230,24 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
         if (live) codes[p.col + k % 8] = (int8_t)(e != e ? 0 : (int)fmin(fmax(e, -128.0), 127.0));
       }
     } else {
-      for (int m = a.row_lanes >> 1; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+      uint32_t row_largest = largest;
+      for (int m = a.row_lanes >> 1; m > 0; m >>= 1) row_largest = max(row_largest, (uint32_t)__shfl_xor((int)row_largest, m));
       if constexpr (kWaves > 1) {
-        if (lane == 0) part[1][wave] = top;
+        if (lane == 0) part[1][wave] = row_largest;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, (float)part[1][wave - w + i]);
+        for (int i = 0; i < kWaves; ++i) row_largest = max(row_largest, (uint32_t)part[1][wave - w + i]);
       }
+      // a NaN, or numbers that float32 may not hold to all their bits: the whole row in double precision
+      const float top = __uint_as_float(row_largest);
       const bool in_float = top >= 0x1p-80f && top <= 0x1p80f;
+      const float from = in_float ? top * (1 - 0x1p-18f) : -1.0f;  // what may be the largest
+      if (!(__uint_as_float(largest) < from))
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s)
+        for (int s = 0; s < kSlots; ++s)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < at[s].count && !(in_float && fabsf(n[s][i]) < top * (1 - 0x1p-18f))) open |= 1u << (8 * s + i);
+          for (int i = 0; i < 8; ++i)
+            if (i < at[s].count && !(fabsf(n[s][i]) < from)) open |= 1u << (8 * s + i);
       double most = 0;
 #pragma unroll 1
       for (; open; open &= open - 1) {
@@ -245,19 +265,21 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
       const bool bad = !__builtin_isfinite(most);
       const double mul = most > 0 && !bad ? 127.0 / most : 0.0;
       if (live && row_lane == 0 && w == 0) a.scales[row] = bad ? __builtin_nanf("") : (float)(most / 127.0);
-      const float mul32 = (float)mul;
+      const float mul32 = in_float ? (float)mul : 0.0f;
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) {
         if (at[s].count <= 0) continue;
         int8_t q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float v = bad ? 0.0f : n[s][i] * mul32 + 0.5f, f = floorf(v);
-          if (!bad && i < at[s].count && !(in_float && v - f > kNear && v - f < 1 - kNear)) open |= 1u << (8 * s + i);
-          q[i] = (int8_t)(int)fminf(fmaxf(f, -127.0f), 127.0f);
+          const float v = __builtin_fmaf(n[s][i], mul32, 0.5f);  // in_float: within -127 .. 128
+          if (i < at[s].count && !decided(v)) open |= 1u << (8 * s + i);
+          q[i] = (int8_t)(in_float ? (int)floorf(v) : 0);
         }
+        if (!in_float) open |= bad ? 0u : ((1u << at[s].count) - 1) << (8 * s);
         store(at[s], q);
       }
+      if (bad) open = 0;
 #pragma unroll 1
       for (; open; open &= open - 1) {
         const int k = __builtin_ctz(open);

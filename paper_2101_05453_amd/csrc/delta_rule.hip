@@ -407,20 +407,204 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
 }
 
 // A workgroup carries kMain * kCols * 16 columns of one head's state through the sequence: kMain waves have 16 kCols columns
-// each, in the registers, for good; four more bring the next chunk's operands into LDS meanwhile, in parts and in the MFMA's
-// order.  kBuffers = 1 where two do not fit.
+// each, in the registers, for good; four more ("loaders") bring the next chunk's operands into LDS meanwhile, in parts and
+// in the MFMA's order, with the chunk after it already requested.  kBuffers = 1 where two do not fit.
 template <class T, int kDk, int kMain, int kCols>
 struct Scan {
-  static constexpr int kP = kParts<T>, kBlocks = kDk / 32, kLoad = 4;
-  static constexpr int kThreads = (kMain + kLoad) * 64;
+  static constexpr int kP = kParts<T>, kBlocks = kDk / 32, kLoaders = 4, kColumns = 16 * kMain * kCols;
+  static constexpr int kThreads = (kMain + kLoaders) * 64;
   struct Buffer {
     u32x4 k[2][kBlocks][kP][64], q[2][kBlocks][kP][64];  // rows of steps, by key column
     u32x4 kt[kDk / 16][kP][64];                          // rows of key columns, by step
     u32x4 x[2][3][64], p[2][3][64];
+    u32x4 vt[kColumns / 16][sizeof(T) / 2][64];          // rows of value columns, by step: as they are
     float factor[4][kChunk];
   };
   static constexpr int kBuffers = 2 * sizeof(Buffer) <= 160 * 1024 ? 2 : 1;
 };
+
+// Where lane (i, g)'s operand lies among the 64 of k, q, kt and vt: the writers, which have four rows of one g each, then
+// meet in no bank, and a reader's order does not matter.
+__device__ inline int slot_of(int i, int g) { return (i ^ g) + 16 * g; }
+
+// A block of four steps x four columns of a matrix [T, width]
+template <class T>
+struct Block4 {
+  Raw4<T> row[4];
+  // four columns from col on, where there are that many; else the last four of the row, which shifted() puts in place
+  __device__ void fetch(const T *p, int64_t stride, int t, int last, int col, int width) {
+    const T *at = p + min(col, width - 4);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) row[r].load(at + (int64_t)min(t + r, last) * stride, 4);
+  }
+  // columns beyond the width as zeros
+  __device__ void shift(int col, int width) {
+    const int s = col - min(col, width - 4);
+    if (s == 0) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      Raw4<T> o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        T v = (T)0.0f;
+#pragma unroll
+        for (int j = i + 1; j < 4; ++j)
+          if (j == i + s) v = row[r].e[j];
+        o.e[i] = v;
+      }
+      row[r] = o;
+    }
+  }
+  // part p of row r, as two words
+  template <int kP>
+  __device__ void parts(int r, uint32_t out[kP][2]) const {
+    if constexpr (kP == 1) {
+      out[0][0] = row[r].w[0], out[0][1] = row[r].w[1];
+    } else {
+      const float x[4] = {(float)row[r].e[0], (float)row[r].e[1], (float)row[r].e[2], (float)row[r].e[3]};
+      parts4<kP>(x, out);
+    }
+  }
+};
+
+// column j of four rows of two words (four 16-bit elements each), as two words
+__device__ inline u32x2_any column_of(const uint32_t w[4][2], int j) {
+  const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;
+  return u32x2_any{__builtin_amdgcn_perm(w[1][j / 2], w[0][j / 2], pick), __builtin_amdgcn_perm(w[3][j / 2], w[2][j / 2], pick)};
+}
+__device__ inline void put8(u32x4 &to, int half, u32x2_any v) { reinterpret_cast<uint64_t *>(&to)[half] = __builtin_bit_cast(uint64_t, v); }
+
+template <class T, int kDk, int kMain, int kCols>
+__device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain, kCols>::Buffer *buffer, int b, int h, int len, int chunks) {
+  using S = Scan<T, kDk, kMain, kCols>;
+  constexpr int kP = S::kP, kHalfWords = sizeof(T) / 2;
+  constexpr int kKeyBlocks = 8 * (kDk / 4), kEach = (kKeyBlocks + 255) / 256, kValueBlocks = 8 * (S::kColumns / 4);
+  const DeltaArgs &d = a.d;
+  const int tid = threadIdx.x - kMain * 64, hk = h / (d.Hv / d.Hk);
+  const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
+  const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
+  const T *vp = static_cast<const T *>(d.v) + b * d.v_stride[1] + h * d.v_stride[2];
+  const float *item = a.items + (int64_t)(b * d.Hv + h) * a.chunks * kItemFloats;
+  // block id: 4 x 16 blocks to a wave, the steps' half above that, then the columns
+  auto step_of = [](int id) { return (id / 64 % 2 * 4 + id % 4) * 4; };
+  auto col_of = [](int id) { return (id / 128 * 16 + id / 4 % 16) * 4; };
+  // fewer than 16 blocks of value columns: the steps' half above them
+  constexpr int kVc = S::kColumns / 4 < 16 ? S::kColumns / 4 : 16;
+  const int v_step = (tid / (4 * kVc) % 2 * 4 + tid % 4) * 4, v_col = (tid / (8 * kVc) * kVc + tid / 4 % kVc) * 4;
+  const int v_from = blockIdx.y * S::kColumns + v_col;
+  struct Stage {
+    Block4<T> k[kEach], q[kEach], v;
+    f32x4 m[2];
+    float f;
+  };
+  auto fetch = [&](Stage &s, int c) {
+    c = min(c, chunks - 1);
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      const int id = kKeyBlocks < 256 ? tid % kKeyBlocks : tid + 256 * n;
+      s.k[n].fetch(kp, d.k_stride[0], c * kChunk + step_of(id), len - 1, col_of(id), d.Dk);
+      s.q[n].fetch(qp, d.q_stride[0], c * kChunk + step_of(id), len - 1, col_of(id), d.Dk);
+    }
+    s.v.fetch(vp, d.v_stride[0], c * kChunk + v_step, len - 1, v_from, d.Dv);
+    const float *it = item + (int64_t)c * kItemFloats;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) s.m[e] = *reinterpret_cast<const f32x4 *>(it + tid * 8 + 4 * e);
+    s.f = it[2 * kMatrix + (tid & 127)];
+  };
+  auto put = [&](Stage &s, typename S::Buffer &o) {
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) {
+      const int id = tid + 256 * n;
+      if (kKeyBlocks < 256 && id >= kKeyBlocks) break;
+      const int step = step_of(id), col = col_of(id), m = step / 16, kb = col / 32, kg = col % 16 / 4, half = col % 32 / 16;
+      s.q[n].shift(col, d.Dk);
+      s.k[n].shift(col, d.Dk);
+      uint32_t w[kP][4][2];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint32_t v[kP][2];
+        s.q[n].template parts<kP>(r, v);
+#pragma unroll
+        for (int p = 0; p < kP; ++p) put8(o.q[m][kb][p][slot_of(step % 16 + r, kg)], half, u32x2_any{v[p][0], v[p][1]});
+        s.k[n].template parts<kP>(r, v);
+#pragma unroll
+        for (int p = 0; p < kP; ++p) {
+          put8(o.k[m][kb][p][slot_of(step % 16 + r, kg)], half, u32x2_any{v[p][0], v[p][1]});
+          w[p][r][0] = v[p][0], w[p][r][1] = v[p][1];
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < kP; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) put8(o.kt[col / 16][p][slot_of(col % 16 + j, step % 16 / 4)], m, column_of(w[p], j));
+    }
+    if (kValueBlocks >= 256 || tid < kValueBlocks) {
+      s.v.shift(v_from, d.Dv);
+      u32x4 *to = &o.vt[v_col / 16][0][0];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int slot = slot_of(v_col % 16 + j, v_step % 16 / 4);
+        if constexpr (kHalfWords == 1) {
+          uint32_t w[4][2];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) w[r][0] = s.v.row[r].w[0], w[r][1] = s.v.row[r].w[1];
+          put8(to[slot], v_step / 16, column_of(w, j));
+        } else {
+          to[v_step / 16 * 64 + slot] = u32x4{s.v.row[0].w[j], s.v.row[1].w[j], s.v.row[2].w[j], s.v.row[3].w[j]};
+        }
+      }
+    }
+    Frag f[3];
+    split8(s.m[0], s.m[1], f);
+    u32x4(*to)[3][64] = tid < 128 ? o.x : o.p;
+#pragma unroll
+    for (int p = 0; p < 3; ++p) to[tid / 64 % 2][p][tid & 63] = f[p].w;
+    if (tid < 128) o.factor[tid / 32][tid % 32] = s.f;
+  };
+  if (chunks == 0) {
+    if constexpr (S::kBuffers == 2) __syncthreads();
+    return;
+  }
+  if constexpr (S::kBuffers == 2) {
+    Stage even, odd;
+    fetch(even, 0);
+    fetch(odd, 1);
+    put(even, buffer[0]);
+    fetch(even, 2);
+    __syncthreads();
+    for (int c = 0;; c += 2) {  // main is at chunk c
+      if (c + 1 < chunks) put(odd, buffer[1]);
+      fetch(odd, c + 3);
+      __syncthreads();
+      if (c + 1 >= chunks) break;
+      if (c + 2 < chunks) put(even, buffer[0]);
+      fetch(even, c + 4);
+      __syncthreads();
+      if (c + 2 >= chunks) break;
+    }
+  } else {
+    Stage s;
+    fetch(s, 0);
+    for (int c = 0; c < chunks; ++c) {
+      put(s, buffer[0]);
+      fetch(s, c + 1);
+      __syncthreads();
+      __syncthreads();
+    }
+  }
+}
+
+// c[n] += a[n] b over the parts that matter, the smallest products first, the chains side by side
+template <int kPa, int kN>
+__device__ inline void mfma_side_by_side(const Frag (*a)[kPa], const Frag *b, f32x4 **c) {
+#pragma unroll
+  for (int i = kPa - 1; i >= 0; --i)
+#pragma unroll
+    for (int j = 2; j >= 0; --j)
+      if (i + j <= 2)
+#pragma unroll
+        for (int n = 0; n < kN; ++n) *c[n] = mfma(a[n][i], b[j], *c[n]);
+}
 
 template <class T, int kDk, int kMain, int kCols>
 __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs a) {
@@ -428,112 +612,15 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
   constexpr int kP = S::kP, kBlocks = S::kBlocks, kBuffers = S::kBuffers;
   const DeltaArgs &d = a.d;
   __shared__ typename S::Buffer buffer[kBuffers];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int i = lane & 15, g = lane >> 4;
-  const int bh = blockIdx.x, b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.x, b = bh / d.Hv, h = bh % d.Hv;
   const int len = length_of(d, b), chunks = (len + kChunk - 1) / kChunk;
+  if (wave >= kMain) return scan_load<T, kDk, kMain, kCols>(a, buffer, b, h, len, chunks);
 
-  if (wave >= kMain) {
-    // blocks of 4 steps x 4 key columns
-    constexpr int kBlocks4 = 8 * (kDk / 4), kEach = (kBlocks4 + 255) / 256;
-    const int tid = threadIdx.x - kMain * 64;
-    const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
-    const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
-    const float *item = a.items + (int64_t)bh * a.chunks * kItemFloats;
-    Raw4<T> rk[kEach][4], rq[kEach][4];
-    f32x4 rm[2];
-    float rf;
-    auto fetch = [&](int c) {
-#pragma unroll
-      for (int n = 0; n < kEach; ++n) {
-        const int id = tid + 256 * n;
-        if (kBlocks4 % 256 && id >= kBlocks4) break;
-        const int step = (id / 64 % 2 * 4 + id % 4) * 4, col = (id / 128 * 16 + id / 4 % 16) * 4;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t t = c * kChunk + step + r;
-          const int there = t < len ? d.Dk - col : 0;
-          rk[n][r].load(kp + t * d.k_stride[0] + col, there);
-          rq[n][r].load(qp + t * d.q_stride[0] + col, there);
-        }
-      }
-      const float *it = item + (int64_t)c * kItemFloats;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) rm[e] = *reinterpret_cast<const f32x4 *>(it + tid * 8 + 4 * e);
-      rf = it[2 * kMatrix + (tid & 127)];
-    };
-    auto put = [&](typename S::Buffer &o) {
-#pragma unroll
-      for (int n = 0; n < kEach; ++n) {
-        const int id = tid + 256 * n;
-        if (kBlocks4 % 256 && id >= kBlocks4) break;
-        const int step = (id / 64 % 2 * 4 + id % 4) * 4, col = (id / 128 * 16 + id / 4 % 16) * 4;
-        const int kb = col / 32, kg = col % 16 / 4, kh = col % 32 / 16;
-        auto words = [&](u32x4 &v, int half) { return reinterpret_cast<uint32_t *>(&v) + 2 * half; };
-        uint32_t w[kP][2];
-        float x[4][4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int m = step / 16, row = step % 16 + r;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[r][j] = (float)rq[n][r].e[j];
-          parts4<kP>(x[r], w);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) {
-            uint32_t *to = words(o.q[m][kb][p][row + 16 * kg], kh);
-            to[0] = w[p][0], to[1] = w[p][1];
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[r][j] = (float)rk[n][r].e[j];
-          parts4<kP>(x[r], w);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) {
-            uint32_t *to = words(o.k[m][kb][p][row + 16 * kg], kh);
-            to[0] = w[p][0], to[1] = w[p][1];
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
-          parts4<kP>(y, w);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) {
-            uint32_t *to = words(o.kt[col / 16][p][col % 16 + j + 16 * (step % 16 / 4)], step / 16);
-            to[0] = w[p][0], to[1] = w[p][1];
-          }
-        }
-      }
-      Frag f[3];
-      split8(rm[0], rm[1], f);
-      u32x4(*to)[3][64] = tid < 128 ? o.x : o.p;
-#pragma unroll
-      for (int p = 0; p < 3; ++p) to[tid / 64 % 2][p][tid & 63] = f[p].w;
-      if (tid < 128) o.factor[tid / 32][tid % 32] = rf;
-    };
-    if (chunks > 0) fetch(0);
-    if constexpr (kBuffers == 2) {
-      if (chunks > 0) put(buffer[0]);
-      if (chunks > 1) fetch(1);
-      __syncthreads();
-      for (int c = 0; c < chunks; ++c) {
-        if (c + 1 < chunks) put(buffer[(c + 1) & 1]);
-        if (c + 2 < chunks) fetch(c + 2);
-        __syncthreads();
-      }
-    } else {
-      for (int c = 0; c < chunks; ++c) {
-        put(buffer[0]);
-        if (c + 1 < chunks) fetch(c + 1);
-        __syncthreads();
-        __syncthreads();
-      }
-    }
-    return;
-  }
-
+  const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, slot = slot_of(i, g);
   int col[kCols];
   f32x4 st[kCols][kDk / 16];
-  const int64_t head = ((int64_t)b * d.Hv + h) * d.Dk * d.Dv;
+  const int64_t head = (int64_t)bh * d.Dk * d.Dv;
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
     col[n] = ((blockIdx.y * kMain + wave) * kCols + n) * 16 + i;
@@ -545,21 +632,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         st[n][m][r] = d.state && row < d.Dk && col[n] < d.Dv ? d.state[head + (int64_t)row * d.Dv + col[n]] : 0.0f;
       }
   }
-  const T *v = static_cast<const T *>(d.v) + b * d.v_stride[1] + h * d.v_stride[2];
   T *y = static_cast<T *>(d.y) + b * d.y_stride[1] + h * d.y_stride[2];
-  T next[kCols][2][4];
-  auto fetch_v = [&](int c) {
-#pragma unroll
-    for (int n = 0; n < kCols; ++n)
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t t = c * kChunk + 16 * m + 4 * g + r;
-          next[n][m][r] = t < len && col[n] < d.Dv ? v[t * d.v_stride[0] + col[n]] : (T)0.0f;
-        }
-  };
-  fetch_v(0);
   if constexpr (kBuffers == 2) __syncthreads();
   for (int c = 0; c < chunks; ++c) {
     if constexpr (kBuffers == 1) __syncthreads();
@@ -571,42 +644,47 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       for (int m = 0; m < 2; ++m) rhs[n][m] = out[n][m] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb) {
-      Frag s[kCols][3], f[kP];
+      Frag f[4][kP];
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) split8(st[n][2 * kb], st[n][2 * kb + 1], s[n]);
+      for (int p = 0; p < kP; ++p) {
+        f[0][p].w = o.k[0][kb][p][slot], f[1][p].w = o.q[0][kb][p][slot];
+        f[2][p].w = o.k[1][kb][p][slot], f[3][p].w = o.q[1][kb][p][slot];
+      }
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-#pragma unroll
-        for (int p = 0; p < kP; ++p) f[p].w = o.k[m][kb][p][lane];
-#pragma unroll
-        for (int n = 0; n < kCols; ++n) rhs[n][m] = mfma_parts<kP, 3>(f, s[n], rhs[n][m]);
-#pragma unroll
-        for (int p = 0; p < kP; ++p) f[p].w = o.q[m][kb][p][lane];
-#pragma unroll
-        for (int n = 0; n < kCols; ++n) out[n][m] = mfma_parts<kP, 3>(f, s[n], out[n][m]);
+      for (int n = 0; n < kCols; ++n) {
+        Frag s[3];
+        split8(st[n][2 * kb], st[n][2 * kb + 1], s);
+        f32x4 *to[4] = {&rhs[n][0], &out[n][0], &rhs[n][1], &out[n][1]};
+        mfma_side_by_side<kP, 4>(f, s, to);
       }
     }
     Frag part[kCols][3], x[2][3];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const f32x4 fk = *reinterpret_cast<const f32x4 *>(&o.factor[0][16 * m + 4 * g]), fq = *reinterpret_cast<const f32x4 *>(&o.factor[1][16 * m + 4 * g]);
-#pragma unroll
-      for (int n = 0; n < kCols; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          rhs[n][m][r] = (float)next[n][m][r] - fk[r] * rhs[n][m][r];
-          out[n][m][r] *= fq[r];
-        }
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int p = 0; p < 3; ++p) x[m][p].w = o.x[m][p][lane];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      Raw8<T> v;
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e) v.w[e] = o.vt[wave * kCols + n][e][slot];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const f32x4 fk = *reinterpret_cast<const f32x4 *>(&o.factor[0][16 * m + 4 * g]), fq = *reinterpret_cast<const f32x4 *>(&o.factor[1][16 * m + 4 * g]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          rhs[n][m][r] = __builtin_fmaf(-fk[r], rhs[n][m][r], (float)v.e[4 * m + r]);
+          out[n][m][r] *= fq[r];
+        }
+      }
     }
-    if (c + 1 < chunks) fetch_v(c + 1);
     f32x4 u[kCols][2];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
       split8(rhs[n][0], rhs[n][1], part[n]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) u[n][m] = mfma_parts<3, 3>(x[m], part[n], f32x4{0, 0, 0, 0});
+      u[n][0] = u[n][1] = f32x4{0, 0, 0, 0};
+      f32x4 *to[2] = {&u[n][0], &u[n][1]};
+      mfma_side_by_side<3, 2>(x, part[n], to);
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -615,8 +693,8 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
       split8(u[n][0], u[n][1], part[n]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) out[n][m] = mfma_parts<3, 3>(x[m], part[n], out[n][m]);
+      f32x4 *to[2] = {&out[n][0], &out[n][1]};
+      mfma_side_by_side<3, 2>(x, part[n], to);
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
@@ -628,22 +706,35 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
 #pragma unroll
     for (int n = 0; n < kCols; ++n) split8(u[n][0], u[n][1], part[n]);
 #pragma unroll
-    for (int m = 0; m < kDk / 16; ++m) {
-      Frag f[kP];
+    for (int m = 0; m < kDk / 16; m += 2) {
+      Frag f[2][kP];
 #pragma unroll
-      for (int p = 0; p < kP; ++p) f[p].w = o.kt[m][p][lane];
+      for (int p = 0; p < kP; ++p) f[0][p].w = o.kt[m][p][slot], f[1][p].w = o.kt[m + 1][p][slot];
 #pragma unroll
-      for (int n = 0; n < kCols; ++n) st[n][m] = mfma_parts<kP, 3>(f, part[n], st[n][m] * whole);
+      for (int n = 0; n < kCols; ++n) {
+        st[n][m] *= whole, st[n][m + 1] *= whole;
+        f32x4 *to[2] = {&st[n][m], &st[n][m + 1]};
+        mfma_side_by_side<kP, 2>(f, part[n], to);
+      }
     }
+    T *yc = y + (int64_t)(c * kChunk + 4 * g) * d.y_stride[0];
+    const int left = len - c * kChunk - 4 * g;  // steps from this lane's first on
 #pragma unroll
-    for (int n = 0; n < kCols; ++n)
+    for (int n = 0; n < kCols; ++n) {
+      if (col[n] >= d.Dv) continue;
+      if (c * kChunk + kChunk <= len) {
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t t = c * kChunk + 16 * m + 4 * g + r;
-          if (t < len && col[n] < d.Dv) y[t * d.y_stride[0] + col[n]] = (T)out[n][m][r];
-        }
+          for (int r = 0; r < 4; ++r) yc[(int64_t)(16 * m + r) * d.y_stride[0] + col[n]] = (T)out[n][m][r];
+      } else {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (16 * m + r < left) yc[(int64_t)(16 * m + r) * d.y_stride[0] + col[n]] = (T)out[n][m][r];
+      }
+    }
     __syncthreads();
   }
   if (!d.new_state) return;
@@ -664,10 +755,20 @@ int launch_scan(const ChunkArgs &a, hipStream_t s) {
   return launch(delta_scan_kernel<T, kDk, kMain, kCols>, grid, dim3((kMain + 4) * 64), s, a);
 }
 
+// As many columns to a workgroup as leave one for each compute unit: their operands come from memory once
 template <class T, int kDk>
 int launch_scan(const ChunkArgs &a, hipStream_t s) {
-  const int64_t tiles = (int64_t)a.d.B * a.d.Hv * ((a.d.Dv + 15) / 16);
-  return tiles >= 1024 ? launch_scan<T, kDk, 4, 1>(a, s) : launch_scan<T, kDk, 1, 1>(a, s);
+  const int64_t heads = (int64_t)a.d.B * a.d.Hv;
+  auto groups = [&](int columns) { return heads * ((a.d.Dv + columns - 1) / columns); };
+  // 256 key columns: the state of 32 value columns and their products' operands are more than a wave has registers, and
+  // in float32 LDS holds a chunk beside 16 value columns only
+  if constexpr (kDk <= 128)
+    if (groups(128) >= 256) return launch_scan<T, kDk, 4, 2>(a, s);
+  if constexpr (kDk <= 128 || sizeof(T) == 2) {
+    if (groups(64) >= 256) return launch_scan<T, kDk, 4, 1>(a, s);
+    if (groups(32) >= 256) return launch_scan<T, kDk, 2, 1>(a, s);
+  }
+  return launch_scan<T, kDk, 1, 1>(a, s);
 }
 
 template <class T>
@@ -677,7 +778,7 @@ int launch_chunks(const ChunkArgs &a, hipStream_t s) {
   return a.d.Dk <= 64 ? launch_scan<T, 64>(a, s) : a.d.Dk <= 128 ? launch_scan<T, 128>(a, s) : launch_scan<T, 256>(a, s);
 }
 
-bool in_chunks(const delta_rule_args *p) { return p->steps >= kChunk; }
+bool in_chunks(const delta_rule_args *p) { return p->steps >= kChunk && p->key_dim >= 4 && p->value_dim >= 4; }
 
 int check(const delta_rule_args *p) {
   if (!p || p->steps < 0 || p->batch < 0 || p->key_heads < 1 || p->value_heads < 1 || p->value_heads % p->key_heads || p->key_dim < 1 ||

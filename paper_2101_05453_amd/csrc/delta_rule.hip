@@ -143,17 +143,26 @@ int launch_step(const DeltaArgs &a, hipStream_t s) {
 // X and P do not depend on the state: delta_prep_kernel computes them for all chunks side by side.  delta_scan_kernel
 // carries the state from chunk to chunk.
 //
-// Products: on the bf16 MFMA, whose products are exact and whose sums are float32.  A float32 operand is taken as three
-// bf16 parts that add up to it exactly (8 + 8 + 8 bits of its 24), and of the products of two operands' parts those are
-// left out that are below 2^-24 of the largest: float32 results at three (a bf16 key with the state) to six MFMAs for
-// one, where the float32 MFMA takes 16 times the time.
+// Products run on the fp16 MFMA, whose products are exact and whose sums are float32.  A float32 operand is scaled by a power
+// of two -- each row of a left operand and each column of a right one by its own -- and taken as two fp16 parts: 22 bits of
+// each element, and 2^-25 of the largest.  Of the products of parts the one of the two low ones, 2^-22 of the others, is
+// left out.  bf16 and fp16 keys and queries are one part.  So results are as exact as float32 products, at two or three
+// MFMAs for one, where the float32 MFMA takes 16 times the time (three bf16 parts, which need no scales, took three to
+// six, and twice the vector instructions for the parts of a state: 2048 steps of 8 x 32 heads 280 us for this kernel).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kChunk = 32;
-constexpr int kMatrix = 2 * 64 * 8;                   // floats of X or P in the workspace: two tiles of 16 rows, 8 floats a lane
-constexpr int kItemFloats = 2 * kMatrix + 4 * kChunk;  // X, P and four factors for each step
+constexpr int kHeadsOfGrid = 1 << 15;  // blockIdx.y of the first kernel, blockIdx.z counts on
+constexpr int kMatrix = 2 * 2 * 64 * 4;  // words of X or P in the workspace: two tiles of 16 rows, two parts, 16 bytes a lane
+// factors of a chunk's steps: of K S, Q S and u for the state; 1 / scale of the rows of X and P; e^c_last; scales of the
+// rows of K and Q
+enum { kFk, kFq, kFu, kFx, kFp, kFwhole, kFactors, kSk = kFactors, kSq, kAllFactors };
+constexpr int kItemWords = 2 * kMatrix + kAllFactors * kChunk;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-template <class T> constexpr int kParts = sizeof(T) == 4 ? 3 : __is_same(T, __bf16) ? 1 : 2;  // bf16 parts of an input
+template <class T> constexpr int kParts = sizeof(T) == 4 ? 2 : 1;  // fp16 parts of a scaled key or query
 
 // The MFMA's operand order: lane (i = lane % 16, g = lane / 16) of a 16 x 32 operand has the columns 4 g .. 4 g + 3 and
 // 16 + 4 g .. 16 + 4 g + 3 of row i.  A result (column lane % 16, rows 4 g .. 4 g + 3) of two 16-row tiles then is the
@@ -161,249 +170,330 @@ template <class T> constexpr int kParts = sizeof(T) == 4 ? 3 : __is_same(T, __bf
 union Frag {
   u32x4 w;
   bf16x8 b;
+  f16x8 h;
 };
 
-__device__ inline f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0); }
 
-__device__ inline uint32_t high_halves(float lo, float hi) {
-  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+// scale and 1 / scale, powers of two, that bring numbers whose largest has these bits (without sign) to 1 .. 2
+struct Scale {
+  float up, down;
+};
+__device__ inline Scale scale_of(uint32_t bits) {
+  bits = min(max(bits & 0x7f800000u, 0x00800000u), 0x7e800000u);
+  return {__uint_as_float(0x7f000000u - bits), __uint_as_float(bits)};
 }
-__device__ inline float truncated(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ inline uint32_t bits_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// the largest over the four lanes of a column
+__device__ inline uint32_t over_column(uint32_t v) {
+  // the swaps exchange rows of 16 lanes (halves of the wave) between two registers: of v and v, each with its neighbour
+  auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(s[0], s[1]);
+  s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(s[0], s[1]);
+}
+__device__ inline float inverse_of_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 
-// x = part 0 + part 1 + part 2, exactly
-__device__ inline void split8(const float *x, Frag out[3]) {
+__device__ inline void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
+  const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
+  const f16x2 l = __builtin_convertvector((f32x2{__builtin_fmaf((float)h[0], -1.0f, a), __builtin_fmaf((float)h[1], -1.0f, b)}), f16x2);
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, l);
+}
+// x = part 0 + part 1, for |x| < 65504
+__device__ inline void split8(f32x4 a, f32x4 b, Frag out[2]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float a = x[2 * i], b = x[2 * i + 1];
-    out[0].w[i] = high_halves(a, b);
-    a -= truncated(a);
-    b -= truncated(b);
-    out[1].w[i] = high_halves(a, b);
-    out[2].w[i] = high_halves(a - truncated(a), b - truncated(b));
+  for (int i = 0; i < 2; ++i) {
+    uint32_t hi, lo;
+    split2(a[2 * i], a[2 * i + 1], hi, lo);
+    out[0].w[i] = hi, out[1].w[i] = lo;
+    split2(b[2 * i], b[2 * i + 1], hi, lo);
+    out[0].w[2 + i] = hi, out[1].w[2 + i] = lo;
   }
 }
-__device__ inline void split8(f32x4 a, f32x4 b, Frag out[3]) {
-  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  split8(x, out);
-}
 
-// four neighbouring elements of a row, zeros behind n
+// four neighbouring elements of a row
 template <class T>
 struct Raw4 {
   union {
     uint32_t w[sizeof(T)];
     T e[4];
   };
-  __device__ void load(const T *p, int n) {
-    if (n >= 4) {
-      if constexpr (sizeof(T) == 4) {
-        const u32x4 v = *reinterpret_cast<const u32x4_any *>(p);
+  __device__ void load(const T *p) {
+    if constexpr (sizeof(T) == 4) {
+      const u32x4 v = *reinterpret_cast<const u32x4_any *>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = v[i];
-      } else {
-        const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
-        w[0] = v[0], w[1] = v[1];
-      }
+      for (int i = 0; i < 4; ++i) w[i] = v[i];
     } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) e[i] = i < n ? p[i] : (T)0.0f;
+      const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
+      w[0] = v[0], w[1] = v[1];
     }
+  }
+  // loaded from column col - by: what belongs at col on, zeros behind it
+  __device__ void shift(int by) {
+    if (by == 0) return;
+    Raw4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      T v = (T)0.0f;
+#pragma unroll
+      for (int j = i + 1; j < 4; ++j)
+        if (j == i + by) v = e[j];
+      o.e[i] = v;
+    }
+    *this = o;
+  }
+  __device__ void keep(bool yes) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = yes ? w[i] : 0u;
   }
 };
 
-// part p of four values, as two words
-template <int kP>
-__device__ inline void parts4(const float *x, uint32_t out[kP][2]) {
+// Rows are read from column min(col, width - 4) on; what was there becomes what is at col, zeros behind the width.  Only
+// widths that are no multiple of four have anything to shift.
+template <class T, int kN>
+__device__ inline void place(Raw4<T> (&rows)[kN], int col, int width) {
+  if (width % 4) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float a = x[2 * i], b = x[2 * i + 1];
+    for (int r = 0; r < kN; ++r) rows[r].shift(col - min(col, width - 4));
+  } else {
 #pragma unroll
-    for (int p = 0; p < kP; ++p) {
-      out[p][i] = high_halves(a, b);
-      a -= truncated(a);
-      b -= truncated(b);
-    }
+    for (int r = 0; r < kN; ++r) rows[r].keep(col < width);
   }
-}
-
-// c += a b over the parts of both that matter
-template <int kPa, int kPb>
-__device__ inline f32x4 mfma_parts(const Frag *a, const Frag *b, f32x4 c) {
-#pragma unroll
-  for (int i = kPa - 1; i >= 0; --i)
-#pragma unroll
-    for (int j = kPb - 1; j >= 0; --j)
-      if (i + j <= 2) c = mfma(a[i], b[j], c);
-  return c;
 }
 
 struct ChunkArgs {
   DeltaArgs d;
-  float *items;  // [B Hv][chunks][kItemFloats]
+  uint32_t *items;  // [B Hv][chunks][kItemWords]
   int chunks;
 };
 
 __device__ inline int length_of(const DeltaArgs &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
 
-// One wave per chunk and value head: X, P and the factors of its steps
-//   e^c_i |k_i|^-1,  e^c_i |q_i|^-1 scale,  e^(c_last - c_i) |k_i|^-1,  e^c_last        (norms: 1 without normalize)
+// products of inputs with each other, unscaled: bf16 and fp16 on their own MFMA; float32 in three bf16 parts that add up to
+// it exactly
 template <class T>
+struct Inputs {
+  static constexpr int kN = sizeof(T) == 4 ? 3 : 1;
+  Frag f[kN];
+  __device__ void set(int half, const Raw4<T> &r) {
+    if constexpr (kN == 1) {
+      f[0].w[2 * half] = r.w[0], f[0].w[2 * half + 1] = r.w[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float a = r.e[2 * i], b = r.e[2 * i + 1];
+#pragma unroll
+        for (int p = 0; p < kN; ++p) {
+          f[p].w[2 * half + i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+          a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+          b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+        }
+      }
+    }
+  }
+  static __device__ f32x4 product(const Inputs &a, const Inputs &b, f32x4 c) {
+#pragma unroll
+    for (int i = kN - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = kN - 1; j >= 0; --j)
+        if (i + j < 3) {
+          if constexpr (__is_same(T, _Float16)) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.f[i].h, b.f[j].h, c, 0, 0, 0);
+          else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.f[i].b, b.f[j].b, c, 0, 0, 0);
+        }
+    return c;
+  }
+};
+
+// One wave per chunk and value head: X, P and the factors of its steps
+template <class T, int kDk, bool kWhole>  // kWhole: key_dim = kDk
 __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
-  constexpr int kP = kParts<T>, kLd = 36;
+  constexpr int kLd = 36, kBlocks = kDk / 32;
   const DeltaArgs &d = a.d;
   __shared__ __attribute__((aligned(16))) float mat[2][kChunk * kLd];  // A, then X; P
   __shared__ double sum_g[kChunk];
   __shared__ float rate[kChunk], norm_k[kChunk], norm_q[kChunk];
   const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
   const int chunk = blockIdx.x;
-  for (int bh = blockIdx.y; bh < d.B * d.Hv; bh += gridDim.y) {
-    const int b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
-    const int t0 = chunk * kChunk, left = length_of(d, b) - t0;  // steps of the row from here on
-    if (left <= 0) continue;
-    __syncthreads();
-    {
-      const int t = lane & 31;
-      double c = 0;
-      float bt = 0;
-      if (t < left) {
-        const float gv = d.g[b * d.g_stride[1] + h * d.g_stride[2] + (int64_t)(t0 + t) * d.g_stride[0]];
-        c = gv < -1000.0f ? -1000.0 : (double)gv;  // e^-1000 is zero; the sum stays a number
-        bt = d.beta[b * d.beta_stride[1] + h * d.beta_stride[2] + (int64_t)(t0 + t) * d.beta_stride[0]];
-      }
-#pragma unroll
-      for (int m = 1; m < 32; m <<= 1) {
-        union { double v; int w[2]; } x, y;
-        x.v = c;
-        y.w[0] = __shfl_up(x.w[0], m, 32);
-        y.w[1] = __shfl_up(x.w[1], m, 32);
-        if (t >= m) c += y.v;
-      }
-      if (lane < 32) sum_g[t] = c, rate[t] = bt;
+  const int bh = blockIdx.z * kHeadsOfGrid + blockIdx.y;
+  if (bh >= d.B * d.Hv) return;
+  const int b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
+  const int t0 = chunk * kChunk, left = length_of(d, b) - t0;  // steps of the row from here on
+  if (left <= 0) return;
+  uint32_t *item = a.items + ((int64_t)bh * a.chunks + chunk) * kItemWords;
+  float *factors = reinterpret_cast<float *>(item + 2 * kMatrix);
+  double c = 0;
+  float bt = 0;
+  {
+    const int t = lane & 31;
+    if (t < left) {
+      const float gv = d.g[b * d.g_stride[1] + h * d.g_stride[2] + (int64_t)(t0 + t) * d.g_stride[0]];
+      c = gv < -1000.0f ? -1000.0 : (double)gv;  // e^-1000 is zero; the sum stays a number
+      bt = d.beta[b * d.beta_stride[1] + h * d.beta_stride[2] + (int64_t)(t0 + t) * d.beta_stride[0]];
     }
-    const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
-    const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
-    f32x4 kk[3] = {}, qk[3] = {};  // tiles (0,0), (1,0), (1,1)
-    float sk[2] = {0, 0}, sq[2] = {0, 0};
-    for (int kb = 0; kb < d.Dk; kb += 32) {
-      Frag kf[2][kP], qf[2][kP];
+  }
+  // rows behind the last step are that step again: their rate of writing is zero
+  const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
+  const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
+  f32x4 kk[3] = {}, qk[3] = {};  // tiles (0,0), (1,0), (1,1)
+  float sk[2] = {0, 0}, sq[2] = {0, 0};
+  uint32_t mk[2] = {0, 0}, mq[2] = {0, 0};
+  constexpr int kAtOnce = kBlocks * sizeof(T) > 4 ? 4 / sizeof(T) : kBlocks;
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int t = 16 * m + i;
-        const bool in = t < left;
-        const T *kr = kp + (int64_t)(t0 + t) * d.k_stride[0], *qr = qp + (int64_t)(t0 + t) * d.q_stride[0];
-        Raw4<T> rk[2], rq[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int col = kb + 16 * e + 4 * g;
-          rk[e].load(kr + col, in ? d.Dk - col : 0);
-          rq[e].load(qr + col, in ? d.Dk - col : 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float x[4], y[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[j] = (float)rk[e].e[j], y[j] = (float)rq[e].e[j];
-            sk[m] = __builtin_fmaf(x[j], x[j], sk[m]);
-            sq[m] = __builtin_fmaf(y[j], y[j], sq[m]);
-          }
-          uint32_t w[kP][2];
-          parts4<kP>(x, w);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) kf[m][p].w[2 * e] = w[p][0], kf[m][p].w[2 * e + 1] = w[p][1];
-          parts4<kP>(y, w);
-#pragma unroll
-          for (int p = 0; p < kP; ++p) qf[m][p].w[2 * e] = w[p][0], qf[m][p].w[2 * e + 1] = w[p][1];
-        }
-      }
-      kk[0] = mfma_parts<kP, kP>(kf[0], kf[0], kk[0]);
-      kk[1] = mfma_parts<kP, kP>(kf[1], kf[0], kk[1]);
-      kk[2] = mfma_parts<kP, kP>(kf[1], kf[1], kk[2]);
-      qk[0] = mfma_parts<kP, kP>(qf[0], kf[0], qk[0]);
-      qk[1] = mfma_parts<kP, kP>(qf[1], kf[0], qk[1]);
-      qk[2] = mfma_parts<kP, kP>(qf[1], kf[1], qk[2]);
-    }
+  for (int kb0 = 0; kb0 < kBlocks; kb0 += kAtOnce) {
+    Raw4<T> rk[kAtOnce][2][2], rq[kAtOnce][2][2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      sk[m] += __shfl_xor(sk[m], 16);
-      sk[m] += __shfl_xor(sk[m], 32);
-      sq[m] += __shfl_xor(sq[m], 16);
-      sq[m] += __shfl_xor(sq[m], 32);
-      if (g == 0) {
-        norm_k[16 * m + i] = d.normalize ? 1.0f / sqrtf(sk[m] + kNormEps) : 1.0f;
-        norm_q[16 * m + i] = (d.normalize ? 1.0f / sqrtf(sq[m] + kNormEps) : 1.0f) * d.scale;
-      }
-    }
-    __syncthreads();
-    float *item = a.items + ((int64_t)bh * a.chunks + chunk) * kItemFloats;
-    if (lane < 32) {
-      float *f = item + 2 * kMatrix;
-      const double c = sum_g[lane], end = sum_g[kChunk - 1];
-      const float e = expf((float)c);
-      f[lane] = e * norm_k[lane];
-      f[kChunk + lane] = e * norm_q[lane];
-      f[2 * kChunk + lane] = expf((float)(end - c)) * norm_k[lane];
-      f[3 * kChunk + lane] = expf((float)end);
+      const int64_t t = t0 + min(16 * m + i, left - 1);
+      const T *kr = kp + t * d.k_stride[0], *qr = qp + t * d.q_stride[0];
+#pragma unroll
+      for (int kb = 0; kb < kAtOnce; ++kb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int at = (kb0 + kb) * 32 + 16 * e, col = kWhole ? at + 4 * g : min(at + 4 * g, d.Dk - 4);
+          rk[kb][m][e].load(kr + col);
+          rq[kb][m][e].load(qr + col);
+        }
     }
 #pragma unroll
-    for (int tile = 0; tile < 3; ++tile) {
-      const int tj = (tile == 2 ? 16 : 0) + i;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int ti = (tile ? 16 : 0) + 4 * g + r;
-        const float e = ti >= tj ? expf((float)(sum_g[ti] - sum_g[tj])) * norm_k[tj] : 0.0f;
-        mat[0][ti * kLd + tj] = ti > tj ? e * kk[tile][r] * norm_k[ti] * rate[ti] : 0.0f;
-        mat[1][ti * kLd + tj] = ti >= tj ? e * qk[tile][r] * norm_q[ti] : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) mat[1][(4 * g + r) * kLd + 16 + i] = 0;
-    __syncthreads();
-    // (1 + A)^-1: the 16 x 16 blocks on the diagonal by substitution, a lane a column; then the one below them
-    {
-      const int blk = g & 1;
-      const float *A = mat[0] + 16 * blk * (kLd + 1);
-      float x[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float s = r == i ? 1.0f : 0.0f;
-#pragma unroll
-        for (int m = 0; m < r; ++m) s = __builtin_fmaf(-A[r * kLd + m], x[m], s);
-        x[r] = s;
-      }
-      __syncthreads();
-      if (g < 2)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mat[0][(16 * blk + r) * kLd + 16 * blk + i] = x[r];
-    }
-    __syncthreads();
-    {
-      f32x4 m1 = {0, 0, 0, 0}, m2 = {0, 0, 0, 0};
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        m1 = __builtin_amdgcn_mfma_f32_16x16x4f32(mat[0][(16 + i) * kLd + 4 * g + r], mat[0][(4 * g + r) * kLd + i], m1, 0, 0, 0);
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        m2 = __builtin_amdgcn_mfma_f32_16x16x4f32(mat[0][(16 + i) * kLd + 16 + 4 * g + r], m1[r], m2, 0, 0, 0);
-      __syncthreads();
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        mat[0][(16 + 4 * g + r) * kLd + i] = -m2[r];
-        mat[0][(4 * g + r) * kLd + 16 + i] = 0;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
+    for (int kb = 0; kb < kAtOnce; ++kb) {
+      Inputs<T> kf[2], qf[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          f32x4 v = *reinterpret_cast<const f32x4 *>(&mat[w][(16 * m + i) * kLd + 16 * e + 4 * g]);
-          if (w == 0) v *= *reinterpret_cast<const f32x4 *>(&rate[16 * e + 4 * g]);
-          *reinterpret_cast<f32x4 *>(item + w * kMatrix + (m * 64 + lane) * 8 + 4 * e) = v;
+          const int col = (kb0 + kb) * 32 + 16 * e + 4 * g;
+          if constexpr (!kWhole) {
+            place(reinterpret_cast<Raw4<T>(&)[1]>(rk[kb][m][e]), col, d.Dk);
+            place(reinterpret_cast<Raw4<T>(&)[1]>(rq[kb][m][e]), col, d.Dk);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = (float)rk[kb][m][e].e[j], y = (float)rq[kb][m][e].e[j];
+            sk[m] = __builtin_fmaf(x, x, sk[m]);
+            sq[m] = __builtin_fmaf(y, y, sq[m]);
+            mk[m] = max(mk[m], bits_of(x));
+            mq[m] = max(mq[m], bits_of(y));
+          }
+          kf[m].set(e, rk[kb][m][e]);
+          qf[m].set(e, rq[kb][m][e]);
         }
+      kk[0] = Inputs<T>::product(kf[0], kf[0], kk[0]);
+      qk[0] = Inputs<T>::product(qf[0], kf[0], qk[0]);
+      kk[1] = Inputs<T>::product(kf[1], kf[0], kk[1]);
+      qk[1] = Inputs<T>::product(qf[1], kf[0], qk[1]);
+      kk[2] = Inputs<T>::product(kf[1], kf[1], kk[2]);
+      qk[2] = Inputs<T>::product(qf[1], kf[1], qk[2]);
+    }
   }
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    union { double v; int w[2]; } x, y;
+    x.v = c;
+    y.w[0] = __shfl_up(x.w[0], m, 32);
+    y.w[1] = __shfl_up(x.w[1], m, 32);
+    if ((lane & 31) >= m) c += y.v;
+  }
+  if (lane < 32) sum_g[lane] = c, rate[lane] = bt;
+  float inv_sk[2], inv_sq[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    sk[m] += __shfl_xor(sk[m], 16);
+    sk[m] += __shfl_xor(sk[m], 32);
+    sq[m] += __shfl_xor(sq[m], 16);
+    sq[m] += __shfl_xor(sq[m], 32);
+    const Scale ks = scale_of(over_column(mk[m])), qs = scale_of(over_column(mq[m]));
+    inv_sk[m] = ks.down, inv_sq[m] = qs.down;
+    if (g == 0) {
+      norm_k[16 * m + i] = d.normalize ? 1.0f / sqrtf(sk[m] + kNormEps) : 1.0f;
+      norm_q[16 * m + i] = (d.normalize ? 1.0f / sqrtf(sq[m] + kNormEps) : 1.0f) * d.scale;
+      factors[kSk * kChunk + 16 * m + i] = ks.up;
+      factors[kSq * kChunk + 16 * m + i] = qs.up;
+    }
+  }
+  __syncthreads();
+  if (g < 2) {  // lane = step
+    const double end = sum_g[kChunk - 1];
+    const float e = expf((float)c), dk = g ? inv_sk[1] : inv_sk[0], dq = g ? inv_sq[1] : inv_sq[0];
+    factors[kFk * kChunk + lane] = e * norm_k[lane] * dk;
+    factors[kFq * kChunk + lane] = e * norm_q[lane] * dq;
+    factors[kFu * kChunk + lane] = expf((float)(end - c)) * norm_k[lane] * dk;
+    factors[kFwhole * kChunk + lane] = expf((float)end);
+  }
+#pragma unroll
+  for (int tile = 0; tile < 3; ++tile) {
+    const int tj = (tile == 2 ? 16 : 0) + i;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int ti = (tile ? 16 : 0) + 4 * g + r;
+      const float e = ti >= tj ? expf((float)(sum_g[ti] - sum_g[tj])) * norm_k[tj] : 0.0f;
+      mat[0][ti * kLd + tj] = ti > tj ? e * kk[tile][r] * norm_k[ti] * rate[ti] : 0.0f;
+      mat[1][ti * kLd + tj] = ti >= tj ? e * qk[tile][r] * norm_q[ti] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) mat[1][(4 * g + r) * kLd + 16 + i] = 0;
+  __syncthreads();
+  // (1 + A)^-1: the 16 x 16 blocks on the diagonal by substitution, a lane a column; then the one below them
+  {
+    const int blk = g & 1;
+    const float *A = mat[0] + 16 * blk * (kLd + 1);
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float s0 = r == i ? 1.0f : 0.0f, s1 = 0;
+#pragma unroll
+      for (int m = 0; m < r; m += 4) {
+        const f32x4 row = *reinterpret_cast<const f32x4 *>(A + r * kLd + m);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+          if (m + n < r) (n % 2 ? s1 : s0) = __builtin_fmaf(-row[n], x[m + n], n % 2 ? s1 : s0);
+      }
+      x[r] = s0 + s1;
+      if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // rows of A are read a few ahead, not all at once
+    }
+    __syncthreads();
+    if (g < 2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mat[0][(16 * blk + r) * kLd + 16 * blk + i] = x[r];
+  }
+  __syncthreads();
+  {
+    f32x4 m1 = {0, 0, 0, 0}, m2 = {0, 0, 0, 0};
+    const f32x4 below = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 4 * g]);
+    const f32x4 last = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 16 + 4 * g]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m1 = __builtin_amdgcn_mfma_f32_16x16x4f32(below[r], mat[0][(4 * g + r) * kLd + i], m1, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m2 = __builtin_amdgcn_mfma_f32_16x16x4f32(last[r], m1[r], m2, 0, 0, 0);
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      mat[0][(16 + 4 * g + r) * kLd + i] = -m2[r];
+      mat[0][(4 * g + r) * kLd + 16 + i] = 0;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      f32x4 v[2];
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        v[e] = *reinterpret_cast<const f32x4 *>(&mat[w][(16 * m + i) * kLd + 16 * e + 4 * g]);
+        if (w == 0) v[e] *= *reinterpret_cast<const f32x4 *>(&rate[16 * e + 4 * g]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = max(most, bits_of(v[e][j]));
+      }
+      const Scale s = scale_of(over_column(most));  // lanes i, i + 16, ...: the row's
+      Frag f[2];
+      split8(v[0] * s.up, v[1] * s.up, f);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) *reinterpret_cast<u32x4 *>(item + w * kMatrix + ((m * 2 + p) * 64 + lane) * 4) = f[p].w;
+      if (g == 0) factors[(w ? kFp : kFx) * kChunk + 16 * m + i] = s.down;
+    }
 }
 
 // A workgroup carries kMain * kCols * 16 columns of one head's state through the sequence: kMain waves have 16 kCols columns
@@ -416,9 +506,9 @@ struct Scan {
   struct Buffer {
     u32x4 k[2][kBlocks][kP][64], q[2][kBlocks][kP][64];  // rows of steps, by key column
     u32x4 kt[kDk / 16][kP][64];                          // rows of key columns, by step
-    u32x4 x[2][3][64], p[2][3][64];
+    u32x4 x[2][2][64], p[2][2][64];
     u32x4 vt[kColumns / 16][sizeof(T) / 2][64];          // rows of value columns, by step: as they are
-    float factor[4][kChunk];
+    float factor[kFactors][kChunk];
   };
   static constexpr int kBuffers = 2 * sizeof(Buffer) <= 160 * 1024 ? 2 : 1;
 };
@@ -427,52 +517,23 @@ struct Scan {
 // meet in no bank, and a reader's order does not matter.
 __device__ inline int slot_of(int i, int g) { return (i ^ g) + 16 * g; }
 
-// A block of four steps x four columns of a matrix [T, width]
-template <class T>
-struct Block4 {
-  Raw4<T> row[4];
-  // four columns from col on, where there are that many; else the last four of the row, which shifted() puts in place
-  __device__ void fetch(const T *p, int64_t stride, int t, int last, int col, int width) {
-    const T *at = p + min(col, width - 4);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) row[r].load(at + (int64_t)min(t + r, last) * stride, 4);
-  }
-  // columns beyond the width as zeros
-  __device__ void shift(int col, int width) {
-    const int s = col - min(col, width - 4);
-    if (s == 0) return;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      Raw4<T> o;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        T v = (T)0.0f;
-#pragma unroll
-        for (int j = i + 1; j < 4; ++j)
-          if (j == i + s) v = row[r].e[j];
-        o.e[i] = v;
-      }
-      row[r] = o;
-    }
-  }
-  // part p of row r, as two words
-  template <int kP>
-  __device__ void parts(int r, uint32_t out[kP][2]) const {
-    if constexpr (kP == 1) {
-      out[0][0] = row[r].w[0], out[0][1] = row[r].w[1];
-    } else {
-      const float x[4] = {(float)row[r].e[0], (float)row[r].e[1], (float)row[r].e[2], (float)row[r].e[3]};
-      parts4<kP>(x, out);
-    }
-  }
-};
-
 // column j of four rows of two words (four 16-bit elements each), as two words
 __device__ inline u32x2_any column_of(const uint32_t w[4][2], int j) {
   const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;
   return u32x2_any{__builtin_amdgcn_perm(w[1][j / 2], w[0][j / 2], pick), __builtin_amdgcn_perm(w[3][j / 2], w[2][j / 2], pick)};
 }
 __device__ inline void put8(u32x4 &to, int half, u32x2_any v) { reinterpret_cast<uint64_t *>(&to)[half] = __builtin_bit_cast(uint64_t, v); }
+
+// four elements times a scale in kP fp16 parts, as two words each
+template <int kP, class T>
+__device__ inline void scaled_parts(const Raw4<T> &r, float s, uint32_t out[kP][2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float a = (float)r.e[2 * i] * s, b = (float)r.e[2 * i + 1] * s;
+    if constexpr (kP == 1) out[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+    else split2(a, b, out[0][i], out[1][i]);
+  }
+}
 
 template <class T, int kDk, int kMain, int kCols>
 __device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain, kCols>::Buffer *buffer, int b, int h, int len, int chunks) {
@@ -484,49 +545,71 @@ __device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain
   const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
   const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
   const T *vp = static_cast<const T *>(d.v) + b * d.v_stride[1] + h * d.v_stride[2];
-  const float *item = a.items + (int64_t)(b * d.Hv + h) * a.chunks * kItemFloats;
-  // block id: 4 x 16 blocks to a wave, the steps' half above that, then the columns
-  auto step_of = [](int id) { return (id / 64 % 2 * 4 + id % 4) * 4; };
-  auto col_of = [](int id) { return (id / 128 * 16 + id / 4 % 16) * 4; };
+  const uint32_t *item = a.items + (int64_t)(b * d.Hv + h) * a.chunks * kItemWords;
+  // blocks of 4 steps x 4 columns: 4 x 16 of them to a wave, the steps' half above that, then the columns
+  const int step = (tid / 64 % 2 * 4 + tid % 4) * 4;
+  auto col_of = [&](int n) { return ((tid + 256 * n) / 128 * 16 + tid / 4 % 16) * 4; };
   // fewer than 16 blocks of value columns: the steps' half above them
   constexpr int kVc = S::kColumns / 4 < 16 ? S::kColumns / 4 : 16;
   const int v_step = (tid / (4 * kVc) % 2 * 4 + tid % 4) * 4, v_col = (tid / (8 * kVc) * kVc + tid / 4 % kVc) * 4;
   const int v_from = blockIdx.y * S::kColumns + v_col;
   struct Stage {
-    Block4<T> k[kEach], q[kEach], v;
-    f32x4 m[2];
+    Raw4<T> k[kEach][4], q[kEach][4], v[4];
+    u32x4 m[2];
+    f32x4 sk, sq;
     float f;
   };
+  // where the first row of a block is in chunk 0, and where the sequence's last row is
+  const T *k_at[kEach], *q_at[kEach], *k_end[kEach], *q_end[kEach];
+#pragma unroll
+  for (int n = 0; n < kEach; ++n) {
+    const int col = min(col_of(n), d.Dk - 4);
+    k_at[n] = kp + step * d.k_stride[0] + col;
+    q_at[n] = qp + step * d.q_stride[0] + col;
+    k_end[n] = kp + (int64_t)(len - 1) * d.k_stride[0] + col;
+    q_end[n] = qp + (int64_t)(len - 1) * d.q_stride[0] + col;
+  }
+  const T *v_at = vp + v_step * d.v_stride[0] + min(v_from, d.Dv - 4), *v_end = vp + (int64_t)(len - 1) * d.v_stride[0] + min(v_from, d.Dv - 4);
+  // rows behind the last step are that step again: one path for all chunks, so that nothing waits for a load but its use
   auto fetch = [&](Stage &s, int c) {
     c = min(c, chunks - 1);
+    const int64_t t = (int64_t)c * kChunk;
+    const int left = len - 1 - c * kChunk;
 #pragma unroll
-    for (int n = 0; n < kEach; ++n) {
-      const int id = kKeyBlocks < 256 ? tid % kKeyBlocks : tid + 256 * n;
-      s.k[n].fetch(kp, d.k_stride[0], c * kChunk + step_of(id), len - 1, col_of(id), d.Dk);
-      s.q[n].fetch(qp, d.q_stride[0], c * kChunk + step_of(id), len - 1, col_of(id), d.Dk);
+    for (int r = 0; r < 4; ++r) {
+      const bool in = step + r <= left;
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        s.k[n][r].load(in ? k_at[n] + (t + r) * d.k_stride[0] : k_end[n]);
+        s.q[n][r].load(in ? q_at[n] + (t + r) * d.q_stride[0] : q_end[n]);
+      }
+      s.v[r].load(v_step + r <= left ? v_at + (t + r) * d.v_stride[0] : v_end);
     }
-    s.v.fetch(vp, d.v_stride[0], c * kChunk + v_step, len - 1, v_from, d.Dv);
-    const float *it = item + (int64_t)c * kItemFloats;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) s.m[e] = *reinterpret_cast<const f32x4 *>(it + tid * 8 + 4 * e);
-    s.f = it[2 * kMatrix + (tid & 127)];
+    const uint32_t *it = item + (int64_t)c * kItemWords;
+    const float *factors = reinterpret_cast<const float *>(it + 2 * kMatrix);
+    s.m[0] = *reinterpret_cast<const u32x4 *>(it + tid * 4);
+    s.m[1] = *reinterpret_cast<const u32x4 *>(it + kMatrix + tid * 4);
+    s.sk = *reinterpret_cast<const f32x4 *>(factors + kSk * kChunk + step);
+    s.sq = *reinterpret_cast<const f32x4 *>(factors + kSq * kChunk + step);
+    s.f = factors[tid % (kFactors * kChunk)];
   };
   auto put = [&](Stage &s, typename S::Buffer &o) {
 #pragma unroll
     for (int n = 0; n < kEach; ++n) {
-      const int id = tid + 256 * n;
-      if (kKeyBlocks < 256 && id >= kKeyBlocks) break;
-      const int step = step_of(id), col = col_of(id), m = step / 16, kb = col / 32, kg = col % 16 / 4, half = col % 32 / 16;
-      s.q[n].shift(col, d.Dk);
-      s.k[n].shift(col, d.Dk);
+      const int col = col_of(n), m = step / 16, kb = col / 32, kg = col % 16 / 4, half = col % 32 / 16;
+      if (col >= kDk) break;
+      if (d.Dk < kDk) {
+        place(s.q[n], col, d.Dk);
+        place(s.k[n], col, d.Dk);
+      }
       uint32_t w[kP][4][2];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         uint32_t v[kP][2];
-        s.q[n].template parts<kP>(r, v);
+        scaled_parts<kP>(s.q[n][r], s.sq[r], v);
 #pragma unroll
         for (int p = 0; p < kP; ++p) put8(o.q[m][kb][p][slot_of(step % 16 + r, kg)], half, u32x2_any{v[p][0], v[p][1]});
-        s.k[n].template parts<kP>(r, v);
+        scaled_parts<kP>(s.k[n][r], s.sk[r], v);
 #pragma unroll
         for (int p = 0; p < kP; ++p) {
           put8(o.k[m][kb][p][slot_of(step % 16 + r, kg)], half, u32x2_any{v[p][0], v[p][1]});
@@ -539,27 +622,24 @@ __device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain
         for (int j = 0; j < 4; ++j) put8(o.kt[col / 16][p][slot_of(col % 16 + j, step % 16 / 4)], m, column_of(w[p], j));
     }
     if (kValueBlocks >= 256 || tid < kValueBlocks) {
-      s.v.shift(v_from, d.Dv);
       u32x4 *to = &o.vt[v_col / 16][0][0];
+      if (d.Dv % 4) place(s.v, v_from, d.Dv);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int slot = slot_of(v_col % 16 + j, v_step % 16 / 4);
         if constexpr (kHalfWords == 1) {
           uint32_t w[4][2];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) w[r][0] = s.v.row[r].w[0], w[r][1] = s.v.row[r].w[1];
+          for (int r = 0; r < 4; ++r) w[r][0] = s.v[r].w[0], w[r][1] = s.v[r].w[1];
           put8(to[slot], v_step / 16, column_of(w, j));
         } else {
-          to[v_step / 16 * 64 + slot] = u32x4{s.v.row[0].w[j], s.v.row[1].w[j], s.v.row[2].w[j], s.v.row[3].w[j]};
+          to[v_step / 16 * 64 + slot] = u32x4{s.v[0].w[j], s.v[1].w[j], s.v[2].w[j], s.v[3].w[j]};
         }
       }
     }
-    Frag f[3];
-    split8(s.m[0], s.m[1], f);
-    u32x4(*to)[3][64] = tid < 128 ? o.x : o.p;
-#pragma unroll
-    for (int p = 0; p < 3; ++p) to[tid / 64 % 2][p][tid & 63] = f[p].w;
-    if (tid < 128) o.factor[tid / 32][tid % 32] = s.f;
+    (&o.x[0][0][0])[tid] = s.m[0];
+    (&o.p[0][0][0])[tid] = s.m[1];
+    if (tid < kFactors * kChunk) o.factor[tid / 32][tid % 32] = s.f;
   };
   if (chunks == 0) {
     if constexpr (S::kBuffers == 2) __syncthreads();
@@ -600,16 +680,33 @@ __device__ inline void mfma_side_by_side(const Frag (*a)[kPa], const Frag *b, f3
 #pragma unroll
   for (int i = kPa - 1; i >= 0; --i)
 #pragma unroll
-    for (int j = 2; j >= 0; --j)
-      if (i + j <= 2)
+    for (int j = 1; j >= 0; --j)
+      if (i + j <= 1)
 #pragma unroll
         for (int n = 0; n < kN; ++n) *c[n] = mfma(a[n][i], b[j], *c[n]);
+}
+
+// the largest of eight
+__device__ inline uint32_t largest8(f32x4 a, f32x4 b) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) m = max(m, max(bits_of(a[r]), bits_of(b[r])));
+  return m;
+}
+
+constexpr uint32_t kLow = 0x41800000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^4, 2^15, infinity
+
+// a power of two that brings numbers whose largest has these bits to 2^10 .. 2^11; with the scale they have already it
+// stays within 2^-100 .. 2^100
+__device__ inline float rescale_of(uint32_t bits, float scale) {
+  const float want = scale_of(bits).up * 0x1p10f;
+  return fminf(fmaxf(want, 0x1p-100f / scale), 0x1p100f / scale);
 }
 
 template <class T, int kDk, int kMain, int kCols>
 __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs a) {
   using S = Scan<T, kDk, kMain, kCols>;
-  constexpr int kP = S::kP, kBlocks = S::kBlocks, kBuffers = S::kBuffers;
+  constexpr int kP = S::kP, kBlocks = S::kBlocks, kBuffers = S::kBuffers, kTiles = kDk / 16;
   const DeltaArgs &d = a.d;
   __shared__ typename S::Buffer buffer[kBuffers];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -619,13 +716,15 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, slot = slot_of(i, g);
   int col[kCols];
-  f32x4 st[kCols][kDk / 16];
+  f32x4 st[kCols][kTiles];  // the state times its column's scale, which changes where the column leaves 2^4 .. 2^15
+  float up[kCols];
   const int64_t head = (int64_t)bh * d.Dk * d.Dv;
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
+    up[n] = 1;
     col[n] = ((blockIdx.y * kMain + wave) * kCols + n) * 16 + i;
 #pragma unroll
-    for (int m = 0; m < kDk / 16; ++m)
+    for (int m = 0; m < kTiles; ++m)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * m + 4 * g + r;
@@ -637,6 +736,23 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
   for (int c = 0; c < chunks; ++c) {
     if constexpr (kBuffers == 1) __syncthreads();
     const typename S::Buffer &o = buffer[kBuffers == 2 ? c & 1 : 0];
+    uint32_t most[kCols];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+      most[n] = 0;
+#pragma unroll
+      for (int m = 0; m < kTiles; m += 2) most[n] = max(most[n], largest8(st[n][m], st[n][m + 1]));
+      most[n] = over_column(most[n]);
+      // in range, or nothing, or nothing that a scale would help
+      const bool fine = most[n] - kLow < kHigh - kLow || most[n] == 0 || most[n] >= kInf;
+      if (__any(!fine)) {
+        const float by = fine ? 1.0f : rescale_of(most[n], up[n]);
+#pragma unroll
+        for (int m = 0; m < kTiles; ++m) st[n][m] *= by;
+        up[n] *= by;
+        most[n] = most[n] < kInf ? __float_as_uint(__uint_as_float(most[n]) * by) : most[n];
+      }
+    }
     f32x4 rhs[kCols][2], out[kCols][2];
 #pragma unroll
     for (int n = 0; n < kCols; ++n)
@@ -652,69 +768,83 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       }
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
-        Frag s[3];
+        Frag s[2];
         split8(st[n][2 * kb], st[n][2 * kb + 1], s);
         f32x4 *to[4] = {&rhs[n][0], &out[n][0], &rhs[n][1], &out[n][1]};
         mfma_side_by_side<kP, 4>(f, s, to);
       }
     }
-    Frag part[kCols][3], x[2][3];
+    auto factor = [&](int f, int m) { return *reinterpret_cast<const f32x4 *>(&o.factor[f][16 * m + 4 * g]); };
+    Frag part[2], x[2][2], p[2][2];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int p = 0; p < 3; ++p) x[m][p].w = o.x[m][p][lane];
+      for (int e = 0; e < 2; ++e) x[m][e].w = o.x[m][e][lane], p[m][e].w = o.p[m][e][lane];
+    const float whole = o.factor[kFwhole][0];
+    f32x4 u[kCols][2];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
+      const float down = inverse_of_power(up[n]);
       Raw8<T> v;
 #pragma unroll
       for (int e = 0; e < (int)sizeof(T) / 2; ++e) v.w[e] = o.vt[wave * kCols + n][e][slot];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        const f32x4 fk = *reinterpret_cast<const f32x4 *>(&o.factor[0][16 * m + 4 * g]), fq = *reinterpret_cast<const f32x4 *>(&o.factor[1][16 * m + 4 * g]);
+        const f32x4 fk = factor(kFk, m) * down, fq = factor(kFq, m) * down;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           rhs[n][m][r] = __builtin_fmaf(-fk[r], rhs[n][m][r], (float)v.e[4 * m + r]);
           out[n][m][r] *= fq[r];
         }
       }
-    }
-    f32x4 u[kCols][2];
-#pragma unroll
-    for (int n = 0; n < kCols; ++n) {
-      split8(rhs[n][0], rhs[n][1], part[n]);
+      // u
+      Scale s = scale_of(over_column(largest8(rhs[n][0], rhs[n][1])));
+      split8(rhs[n][0] * s.up, rhs[n][1] * s.up, part);
       u[n][0] = u[n][1] = f32x4{0, 0, 0, 0};
       f32x4 *to[2] = {&u[n][0], &u[n][1]};
-      mfma_side_by_side<3, 2>(x, part[n], to);
+      mfma_side_by_side<2, 2>(x, part, to);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) u[n][m] *= factor(kFx, m) * s.down;
+      // P u
+      s = scale_of(over_column(largest8(u[n][0], u[n][1])));
+      split8(u[n][0] * s.up, u[n][1] * s.up, part);
+      f32x4 pu[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      f32x4 *to2[2] = {&pu[0], &pu[1]};
+      mfma_side_by_side<2, 2>(p, part, to2);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const f32x4 fp = factor(kFp, m) * s.down;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[n][m][r] = __builtin_fmaf(pu[m][r], fp[r], out[n][m][r]);
+        u[n][m] *= factor(kFu, m) * up[n];
+      }
     }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int p = 0; p < 3; ++p) x[m][p].w = o.p[m][p][lane];
+    // the state: what is added has the state's scale, or changes it
+    Frag added[kCols][2];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
-      split8(u[n][0], u[n][1], part[n]);
-      f32x4 *to[2] = {&out[n][0], &out[n][1]};
-      mfma_side_by_side<3, 2>(x, part[n], to);
+      const uint32_t wm = over_column(largest8(u[n][0], u[n][1]));
+      const uint32_t kept = __float_as_uint(__uint_as_float(most[n]) * whole), both = max(wm, kept);
+      const bool fine = wm >= kInf || kept >= kInf || wm == 0 || (wm < kHigh && both >= kLow);
+      if (__any(!fine)) {
+        const float by = fine ? 1.0f : rescale_of(both, up[n]);
+#pragma unroll
+        for (int m = 0; m < kTiles; ++m) st[n][m] *= by;
+        u[n][0] *= by, u[n][1] *= by;
+        up[n] *= by;
+      }
+      split8(u[n][0], u[n][1], added[n]);
     }
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const f32x4 fu = *reinterpret_cast<const f32x4 *>(&o.factor[2][16 * m + 4 * g]);
-#pragma unroll
-      for (int n = 0; n < kCols; ++n) u[n][m] *= fu;
-    }
-    const float whole = o.factor[3][0];
-#pragma unroll
-    for (int n = 0; n < kCols; ++n) split8(u[n][0], u[n][1], part[n]);
-#pragma unroll
-    for (int m = 0; m < kDk / 16; m += 2) {
+    for (int m = 0; m < kTiles; m += 2) {
       Frag f[2][kP];
 #pragma unroll
-      for (int p = 0; p < kP; ++p) f[0][p].w = o.kt[m][p][slot], f[1][p].w = o.kt[m + 1][p][slot];
+      for (int e = 0; e < kP; ++e) f[0][e].w = o.kt[m][e][slot], f[1][e].w = o.kt[m + 1][e][slot];
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
         st[n][m] *= whole, st[n][m + 1] *= whole;
         f32x4 *to[2] = {&st[n][m], &st[n][m + 1]};
-        mfma_side_by_side<kP, 2>(f, part[n], to);
+        mfma_side_by_side<kP, 2>(f, added[n], to);
       }
     }
     T *yc = y + (int64_t)(c * kChunk + 4 * g) * d.y_stride[0];
@@ -739,14 +869,16 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
   }
   if (!d.new_state) return;
 #pragma unroll
-  for (int n = 0; n < kCols; ++n)
+  for (int n = 0; n < kCols; ++n) {
+    const float down = inverse_of_power(up[n]);
 #pragma unroll
-    for (int m = 0; m < kDk / 16; ++m)
+    for (int m = 0; m < kTiles; ++m)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * m + 4 * g + r;
-        if (row < d.Dk && col[n] < d.Dv) d.new_state[head + (int64_t)row * d.Dv + col[n]] = st[n][m][r];
+        if (row < d.Dk && col[n] < d.Dv) d.new_state[head + (int64_t)row * d.Dv + col[n]] = st[n][m][r] * down;
       }
+  }
 }
 
 template <class T, int kDk, int kMain, int kCols>
@@ -771,11 +903,18 @@ int launch_scan(const ChunkArgs &a, hipStream_t s) {
   return launch_scan<T, kDk, 1, 1>(a, s);
 }
 
+template <class T, int kDk>
+int launch_chunks(const ChunkArgs &a, hipStream_t s) {
+  const int heads = a.d.B * a.d.Hv;
+  const dim3 grid(a.chunks, std::min(heads, kHeadsOfGrid), (heads + kHeadsOfGrid - 1) / kHeadsOfGrid);
+  const int rc = a.d.Dk == kDk ? launch(delta_prep_kernel<T, kDk, true>, grid, dim3(64), s, a)
+                               : launch(delta_prep_kernel<T, kDk, false>, grid, dim3(64), s, a);
+  return rc != LSTM_INT_OK ? rc : launch_scan<T, kDk>(a, s);
+}
+
 template <class T>
 int launch_chunks(const ChunkArgs &a, hipStream_t s) {
-  const int rc = launch(delta_prep_kernel<T>, dim3(a.chunks, std::min(a.d.B * a.d.Hv, 65535)), dim3(64), s, a);
-  if (rc != LSTM_INT_OK) return rc;
-  return a.d.Dk <= 64 ? launch_scan<T, 64>(a, s) : a.d.Dk <= 128 ? launch_scan<T, 128>(a, s) : launch_scan<T, 256>(a, s);
+  return a.d.Dk <= 64 ? launch_chunks<T, 64>(a, s) : a.d.Dk <= 128 ? launch_chunks<T, 128>(a, s) : launch_chunks<T, 256>(a, s);
 }
 
 bool in_chunks(const delta_rule_args *p) { return p->steps >= kChunk && p->key_dim >= 4 && p->value_dim >= 4; }
@@ -798,7 +937,7 @@ extern "C" {
 
 size_t delta_rule_workspace_bytes(const delta_rule_args *p) {
   if (check(p) != LSTM_INT_OK || !in_chunks(p)) return 0;
-  return (size_t)p->batch * p->value_heads * ((p->steps + kChunk - 1) / kChunk) * kItemFloats * sizeof(float);
+  return (size_t)p->batch * p->value_heads * ((p->steps + kChunk - 1) / kChunk) * kItemWords * sizeof(uint32_t);
 }
 
 int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, const void *k, const void *v, const float *g,
@@ -823,7 +962,7 @@ int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, 
   if (!scope.ok) return LSTM_INT_E_DEVICE;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   if (in_chunks(p)) {
-    const ChunkArgs c{a, static_cast<float *>(workspace), (p->steps + kChunk - 1) / kChunk};
+    const ChunkArgs c{a, static_cast<uint32_t *>(workspace), (p->steps + kChunk - 1) / kChunk};
     return p->dtype == LM_F32 ? launch_chunks<float>(c, s) : p->dtype == LM_F16 ? launch_chunks<_Float16>(c, s) : launch_chunks<__bf16>(c, s);
   }
   return p->dtype == LM_F32 ? launch_step<float>(a, s) : p->dtype == LM_F16 ? launch_step<_Float16>(a, s) : launch_step<__bf16>(a, s);

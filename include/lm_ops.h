@@ -143,16 +143,16 @@ void w4_linear_destroy(w4_linear_model *model);
  * (' is the transpose; g the log of the decay, beta the rate of writing).  Key
  * head h serves the value heads h * value_heads / key_heads and the ones behind
  * it.  normalize = 1: k and q are first divided by sqrt(sum of squares + 1e-6).
- * Sums and the state are float32; sequences run 64 steps at a time, and their
- * products on the matrix cores take float32 operands in parts of bfloat16 that
- * add up to them, so that results are as exact as float32 products.
+ * Sums and the state are float32; calls of 12 steps and more run 32 steps at a
+ * time on the matrix cores, with float32 operands in two scaled parts of fp16,
+ * 22 bits, so that results are as exact as float32 products.
  *   q, k    DEVICE dtype [T, B, key_heads, key_dim]
  *   v, y    DEVICE dtype [T, B, value_heads, value_dim]
  *   g, beta DEVICE float32 [T, B, value_heads]
  *           each with strides, in elements, of step, batch row and head, that
  *           may be anything for the inputs (a slice of a projection's output);
  *           the last dimension of q, k, v, y is dense.
- *           g = -infinity clears the state.
+ *           g = -infinity clears the state (of finite numbers).
  *   lengths DEVICE int32 [B]: row b has min(max(lengths[b], 0), T) steps; inputs
  *           behind them are not used and outputs there left as they are;
  *           NULL: every row has T
@@ -161,8 +161,8 @@ void w4_linear_destroy(w4_linear_model *model);
  *           kept); may be the same
  *   workspace DEVICE, >= delta_rule_workspace_bytes, 256-byte aligned (may be
  *           NULL if that is 0)
- * A NaN or an infinity at one step can reach the outputs of the steps before it
- * within the same 64.
+ * A NaN or an infinity at one step can reach the outputs of its row and head at
+ * the steps before it within the same 32; nothing reaches another row or head.
  * T = 0 copies the state; B = 0 is a no-op.
  * LSTM_INT_E_INVALID_ARG: NULL, a negative extent, value_heads no multiple of
  * key_heads, an unknown dtype, a normalize other than 0 and 1.  LSTM_INT_E_BAD_RANGE: a scale that is not finite.

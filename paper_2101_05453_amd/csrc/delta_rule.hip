@@ -194,20 +194,26 @@ __device__ inline uint32_t over_column(uint32_t v) {
 }
 __device__ inline float inverse_of_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 
-__device__ inline void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
+// -1 in a register, which the compiler does not see through: a - h is then one instruction that takes the half as it is
+__device__ inline float minus_one() {
+  float v;
+  asm("v_mov_b32 %0, -1.0" : "=v"(v));
+  return v;
+}
+__device__ inline void split2(float a, float b, uint32_t &hi, uint32_t &lo, float minus) {
   const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
-  const f16x2 l = __builtin_convertvector((f32x2{__builtin_fmaf((float)h[0], -1.0f, a), __builtin_fmaf((float)h[1], -1.0f, b)}), f16x2);
+  const f16x2 l = __builtin_convertvector((f32x2{__builtin_fmaf((float)h[0], minus, a), __builtin_fmaf((float)h[1], minus, b)}), f16x2);
   hi = __builtin_bit_cast(uint32_t, h);
   lo = __builtin_bit_cast(uint32_t, l);
 }
 // x = part 0 + part 1, for |x| < 65504
-__device__ inline void split8(f32x4 a, f32x4 b, Frag out[2]) {
+__device__ inline void split8(f32x4 a, f32x4 b, Frag out[2], float minus) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     uint32_t hi, lo;
-    split2(a[2 * i], a[2 * i + 1], hi, lo);
+    split2(a[2 * i], a[2 * i + 1], hi, lo, minus);
     out[0].w[i] = hi, out[1].w[i] = lo;
-    split2(b[2 * i], b[2 * i + 1], hi, lo);
+    split2(b[2 * i], b[2 * i + 1], hi, lo, minus);
     out[0].w[2 + i] = hi, out[1].w[2 + i] = lo;
   }
 }
@@ -489,7 +495,7 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
       }
       const Scale s = scale_of(over_column(most));  // lanes i, i + 16, ...: the row's
       Frag f[2];
-      split8(v[0] * s.up, v[1] * s.up, f);
+      split8(v[0] * s.up, v[1] * s.up, f, minus_one());
 #pragma unroll
       for (int p = 0; p < 2; ++p) *reinterpret_cast<u32x4 *>(item + w * kMatrix + ((m * 2 + p) * 64 + lane) * 4) = f[p].w;
       if (g == 0) factors[(w ? kFp : kFx) * kChunk + 16 * m + i] = s.down;
@@ -531,7 +537,7 @@ __device__ inline void scaled_parts(const Raw4<T> &r, float s, uint32_t out[kP][
   for (int i = 0; i < 2; ++i) {
     const float a = (float)r.e[2 * i] * s, b = (float)r.e[2 * i + 1] * s;
     if constexpr (kP == 1) out[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
-    else split2(a, b, out[0][i], out[1][i]);
+    else split2(a, b, out[0][i], out[1][i], minus_one());
   }
 }
 
@@ -575,15 +581,25 @@ __device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain
     c = min(c, chunks - 1);
     const int64_t t = (int64_t)c * kChunk;
     const int left = len - 1 - c * kChunk;
+    const T *k_row[kEach], *q_row[kEach], *v_row = v_at + t * d.v_stride[0];
+#pragma unroll
+    for (int n = 0; n < kEach; ++n) k_row[n] = k_at[n] + t * d.k_stride[0], q_row[n] = q_at[n] + t * d.q_stride[0];
+    // a selected address, not a branch around two loads
+    auto either = [](bool yes, const T *a, const T *b) {
+      uint64_t at = reinterpret_cast<uint64_t>(a);
+      asm volatile("" : "+v"(at));
+      at = yes ? at : reinterpret_cast<uint64_t>(b);
+      return (const T *)reinterpret_cast<const __attribute__((address_space(1))) T *>(at);
+    };
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const bool in = step + r <= left;
 #pragma unroll
       for (int n = 0; n < kEach; ++n) {
-        s.k[n][r].load(in ? k_at[n] + (t + r) * d.k_stride[0] : k_end[n]);
-        s.q[n][r].load(in ? q_at[n] + (t + r) * d.q_stride[0] : q_end[n]);
+        s.k[n][r].load(either(in, k_row[n] + r * d.k_stride[0], k_end[n]));
+        s.q[n][r].load(either(in, q_row[n] + r * d.q_stride[0], q_end[n]));
       }
-      s.v[r].load(v_step + r <= left ? v_at + (t + r) * d.v_stride[0] : v_end);
+      s.v[r].load(either(v_step + r <= left, v_row + r * d.v_stride[0], v_end));
     }
     const uint32_t *it = item + (int64_t)c * kItemWords;
     const float *factors = reinterpret_cast<const float *>(it + 2 * kMatrix);
@@ -652,15 +668,15 @@ __device__ inline void scan_load(const ChunkArgs &a, typename Scan<T, kDk, kMain
     put(even, buffer[0]);
     fetch(even, 2);
     __syncthreads();
-    for (int c = 0;; c += 2) {  // main is at chunk c
-      if (c + 1 < chunks) put(odd, buffer[1]);
+    // Two chunks at a time, without a branch: behind the end the last chunk comes again, into the buffer that nobody reads.
+    // (With the branches, waits for one stage's loads became waits for the other's too.)
+    for (int c = 0; c < chunks; c += 2) {  // main is at chunk c
+      put(odd, buffer[1]);
       fetch(odd, c + 3);
       __syncthreads();
-      if (c + 1 >= chunks) break;
-      if (c + 2 < chunks) put(even, buffer[0]);
+      put(even, buffer[0]);
       fetch(even, c + 4);
       __syncthreads();
-      if (c + 2 >= chunks) break;
     }
   } else {
     Stage s;
@@ -686,13 +702,13 @@ __device__ inline void mfma_side_by_side(const Frag (*a)[kPa], const Frag *b, f3
         for (int n = 0; n < kN; ++n) *c[n] = mfma(a[n][i], b[j], *c[n]);
 }
 
-// the largest of eight
-__device__ inline uint32_t largest8(f32x4 a, f32x4 b) {
-  uint32_t m = 0;
+// the largest |x| of eight and m; a NaN is passed over, and comes out of the products by itself
+__device__ inline float largest8(f32x4 a, f32x4 b, float m) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) m = max(m, max(bits_of(a[r]), bits_of(b[r])));
+  for (int r = 0; r < 4; ++r) m = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(a[r]), __builtin_fabsf(b[r])), m);
   return m;
 }
+__device__ inline uint32_t over_column(float m) { return over_column(__float_as_uint(m)); }
 
 constexpr uint32_t kLow = 0x41800000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^4, 2^15, infinity
 
@@ -715,6 +731,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
   if (wave >= kMain) return scan_load<T, kDk, kMain, kCols>(a, buffer, b, h, len, chunks);
 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, slot = slot_of(i, g);
+  const float minus = minus_one();
   int col[kCols];
   f32x4 st[kCols][kTiles];  // the state times its column's scale, which changes where the column leaves 2^4 .. 2^15
   float up[kCols];
@@ -739,10 +756,10 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
     uint32_t most[kCols];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
-      most[n] = 0;
+      float top = 0;
 #pragma unroll
-      for (int m = 0; m < kTiles; m += 2) most[n] = max(most[n], largest8(st[n][m], st[n][m + 1]));
-      most[n] = over_column(most[n]);
+      for (int m = 0; m < kTiles; m += 2) top = largest8(st[n][m], st[n][m + 1], top);
+      most[n] = over_column(top);
       // in range, or nothing, or nothing that a scale would help
       const bool fine = most[n] - kLow < kHigh - kLow || most[n] == 0 || most[n] >= kInf;
       if (__any(!fine)) {
@@ -769,7 +786,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
         Frag s[2];
-        split8(st[n][2 * kb], st[n][2 * kb + 1], s);
+        split8(st[n][2 * kb], st[n][2 * kb + 1], s, minus);
         f32x4 *to[4] = {&rhs[n][0], &out[n][0], &rhs[n][1], &out[n][1]};
         mfma_side_by_side<kP, 4>(f, s, to);
       }
@@ -798,16 +815,16 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         }
       }
       // u
-      Scale s = scale_of(over_column(largest8(rhs[n][0], rhs[n][1])));
-      split8(rhs[n][0] * s.up, rhs[n][1] * s.up, part);
+      Scale s = scale_of(over_column(largest8(rhs[n][0], rhs[n][1], 0.0f)));
+      split8(rhs[n][0] * s.up, rhs[n][1] * s.up, part, minus);
       u[n][0] = u[n][1] = f32x4{0, 0, 0, 0};
       f32x4 *to[2] = {&u[n][0], &u[n][1]};
       mfma_side_by_side<2, 2>(x, part, to);
 #pragma unroll
       for (int m = 0; m < 2; ++m) u[n][m] *= factor(kFx, m) * s.down;
       // P u
-      s = scale_of(over_column(largest8(u[n][0], u[n][1])));
-      split8(u[n][0] * s.up, u[n][1] * s.up, part);
+      s = scale_of(over_column(largest8(u[n][0], u[n][1], 0.0f)));
+      split8(u[n][0] * s.up, u[n][1] * s.up, part, minus);
       f32x4 pu[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
       f32x4 *to2[2] = {&pu[0], &pu[1]};
       mfma_side_by_side<2, 2>(p, part, to2);
@@ -823,7 +840,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
     Frag added[kCols][2];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
-      const uint32_t wm = over_column(largest8(u[n][0], u[n][1]));
+      const uint32_t wm = over_column(largest8(u[n][0], u[n][1], 0.0f));
       const uint32_t kept = __float_as_uint(__uint_as_float(most[n]) * whole), both = max(wm, kept);
       const bool fine = wm >= kInf || kept >= kInf || wm == 0 || (wm < kHigh && both >= kLow);
       if (__any(!fine)) {
@@ -833,7 +850,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         u[n][0] *= by, u[n][1] *= by;
         up[n] *= by;
       }
-      split8(u[n][0], u[n][1], added[n]);
+      split8(u[n][0], u[n][1], added[n], minus);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; m += 2) {
@@ -867,6 +884,8 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
     }
     __syncthreads();
   }
+  if constexpr (kBuffers == 2)
+    if (chunks % 2) __syncthreads();  // the loaders go two chunks at a time
   if (!d.new_state) return;
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
@@ -917,7 +936,9 @@ int launch_chunks(const ChunkArgs &a, hipStream_t s) {
   return a.d.Dk <= 64 ? launch_chunks<T, 64>(a, s) : a.d.Dk <= 128 ? launch_chunks<T, 128>(a, s) : launch_chunks<T, 256>(a, s);
 }
 
-bool in_chunks(const delta_rule_args *p) { return p->steps >= kChunk && p->key_dim >= 4 && p->value_dim >= 4; }
+// A chunk takes the time of some twelve steps: 16 heads of 128 x 128, 8, 12 and 16 steps: 18, 24 and 31 us step by step, 20,
+// 22 and 21 in one chunk; with 64 rows 74, 97 and 121, and 91, 93 and 93.  The loads of a chunk take four columns at once.
+bool in_chunks(const delta_rule_args *p) { return p->steps >= 12 && p->key_dim >= 4 && p->value_dim >= 4; }
 
 int check(const delta_rule_args *p) {
   if (!p || p->steps < 0 || p->batch < 0 || p->key_heads < 1 || p->value_heads < 1 || p->value_heads % p->key_heads || p->key_dim < 1 ||

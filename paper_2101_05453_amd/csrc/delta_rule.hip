@@ -713,10 +713,10 @@ __device__ inline uint32_t over_column(float m) { return over_column(__float_as_
 constexpr uint32_t kLow = 0x41800000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^4, 2^15, infinity
 
 // a power of two that brings numbers whose largest has these bits to 2^10 .. 2^11; with the scale they have already it
-// stays within 2^-100 .. 2^100
+// stays within 2^-120 .. 2^120
 __device__ inline float rescale_of(uint32_t bits, float scale) {
   const float want = scale_of(bits).up * 0x1p10f;
-  return fminf(fmaxf(want, 0x1p-100f / scale), 0x1p100f / scale);
+  return fminf(fmaxf(want, 0x1p-120f / scale), 0x1p120f / scale);
 }
 
 template <class T, int kDk, int kMain, int kCols>

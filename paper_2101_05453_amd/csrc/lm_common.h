@@ -19,6 +19,7 @@ struct DeviceScope {
       return;
     }
     ok = changed = hipSetDevice(device) == hipSuccess;
+    if (!ok) (void)hipGetLastError();  // said by the call's code, not by a later call's
   }
   ~DeviceScope() {
     if (changed) (void)hipSetDevice(prev);
@@ -31,8 +32,9 @@ int launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s, A... args
   static_assert(sizeof...(P) == sizeof...(A), "one argument for each parameter");
   return [&](P... typed) {
     void *ptrs[] = {&typed...};
-    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, block, ptrs, 0, s) == hipSuccess ? LSTM_INT_OK
-                                                                                                         : LSTM_INT_E_DEVICE;
+    if (hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, block, ptrs, 0, s) == hipSuccess) return LSTM_INT_OK;
+    (void)hipGetLastError();
+    return LSTM_INT_E_DEVICE;
   }(args...);
 }
 

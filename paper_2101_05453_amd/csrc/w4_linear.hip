@@ -40,7 +40,7 @@ struct W4Args {
   void *y;
   int64_t x_stride, y_stride;
   int M, N, K, tiles, chunks, groups;  // groups: of all chunks
-  int zero_point, split;
+  int zero_point, split, across;  // across: workgroups over the outputs; blockIdx.x goes over them first
   float scale;
 };
 
@@ -168,9 +168,9 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
   constexpr int kAhead = kRows == 4 ? 2 : 4, per_chunk = kChunk / kGroup;
   __shared__ f32x4 part[8][kRows][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tile = blockIdx.x * (8 / a.split) + wave / a.split, p = wave % a.split;
+  const int tile = blockIdx.x % a.across * (8 / a.split) + wave / a.split, p = wave % a.split;
   const int kg = lane >> 4;
-  const int64_t m0 = (int64_t)blockIdx.y * 16 * kRows + (lane & 15);
+  const int64_t m0 = (int64_t)(blockIdx.x / a.across) * 16 * kRows + (lane & 15);
   f32x4 acc[kRows] = {};
   if (tile < a.tiles) {
     const int8_t *xrow[kRows];
@@ -226,18 +226,19 @@ __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   __shared__ f32x4 ss[2][8 * per_chunk * 4];
   __shared__ u32x4 zs[2][8 * per_chunk * 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, i16 = lane & 15;
-  const int64_t m0 = (int64_t)blockIdx.y * 128;
-  const int nt0 = (wave & 3) * 2, mt0 = (wave >> 2) * 4, tile0 = blockIdx.x * 8 + nt0;
+  const int nb = blockIdx.x % a.across;
+  const int64_t m0 = (int64_t)(blockIdx.x / a.across) * 128;
+  const int nt0 = (wave & 3) * 2, mt0 = (wave >> 2) * 4, tile0 = nb * 8 + nt0;
 
   // a wave brings row tile `wave` and output tile `wave`
   const int64_t mine = m0 + wave * 16 + i16;
   const int8_t *xrow = a.x + (mine < a.M ? mine : a.M - 1) * a.x_stride;
-  const u32x4 *w = reinterpret_cast<const u32x4 *>(a.w) + (int64_t)(blockIdx.x * 8 + wave) * a.chunks * 64;
+  const u32x4 *w = reinterpret_cast<const u32x4 *>(a.w) + (int64_t)(nb * 8 + wave) * a.chunks * 64;
   // scales and sums: the first threads hold one vector each, the others fetch one of those too (no branch around a load)
   constexpr int kS = 8 * per_chunk * 4, kZ = 8 * per_chunk * 2;
   const int st = tid % kS, zt = tid % kZ;
-  const f32x4 *sp = reinterpret_cast<const f32x4 *>(a.s) + ((int64_t)(blockIdx.x * 8 + st / (per_chunk * 4)) * a.groups * 4 + st % (per_chunk * 4));
-  const u32x4 *zp = reinterpret_cast<const u32x4 *>(a.sums) + ((int64_t)(blockIdx.x * 8 + zt / (per_chunk * 2)) * a.groups * 2 + zt % (per_chunk * 2));
+  const f32x4 *sp = reinterpret_cast<const f32x4 *>(a.s) + ((int64_t)(nb * 8 + st / (per_chunk * 4)) * a.groups * 4 + st % (per_chunk * 4));
+  const u32x4 *zp = reinterpret_cast<const u32x4 *>(a.sums) + ((int64_t)(nb * 8 + zt / (per_chunk * 2)) * a.groups * 2 + zt % (per_chunk * 2));
   RowOperands<64> xr;
   u32x4 wr, zr;
   f32x4 sr;
@@ -310,13 +311,17 @@ __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
 }
 
 template <int kGroup, bool kZero, class T>
-int launch_w4(const W4Args &a, hipStream_t s) {
-  if (a.M > 64 && a.chunks > 1) return launch(w4_block_kernel<kGroup, kZero, T>, dim3((a.tiles + 7) / 8, (a.M + 127) / 128), dim3(512), s, a);
-  const int per_block = 8 / a.split;
-  const dim3 grid((a.tiles + per_block - 1) / per_block, a.M <= 32 ? 1 : (a.M + 63) / 64), block(512);
-  return a.M <= 16   ? launch(w4_rows_kernel<kGroup, 1, kZero, T>, grid, block, s, a)
-         : a.M <= 32 ? launch(w4_rows_kernel<kGroup, 2, kZero, T>, grid, block, s, a)
-                     : launch(w4_rows_kernel<kGroup, 4, kZero, T>, grid, block, s, a);
+int launch_w4(W4Args a, hipStream_t s) {
+  const bool blocks = a.M > 64 && a.chunks > 1;
+  const int rows = blocks ? 128 : a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64, tiles = blocks ? 8 : 8 / a.split;
+  a.across = (a.tiles + tiles - 1) / tiles;
+  const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536
+  if (count >= (int64_t)1 << 31) return LSTM_INT_E_UNSUPPORTED;
+  const dim3 grid((unsigned)count), block(512);
+  return blocks       ? launch(w4_block_kernel<kGroup, kZero, T>, grid, block, s, a)
+         : rows == 16 ? launch(w4_rows_kernel<kGroup, 1, kZero, T>, grid, block, s, a)
+         : rows == 32 ? launch(w4_rows_kernel<kGroup, 2, kZero, T>, grid, block, s, a)
+                      : launch(w4_rows_kernel<kGroup, 4, kZero, T>, grid, block, s, a);
 }
 
 template <int kGroup, class T>
@@ -428,6 +433,7 @@ int w4_linear_prepare(const w4_linear_params *p, int32_t device, w4_linear_model
       if (!scope.ok) rc = LSTM_INT_E_DEVICE;
       else if (hipMalloc(reinterpret_cast<void **>(&m->base), img.size()) != hipSuccess) {
         m->base = nullptr;
+        (void)hipGetLastError();  // said here
         rc = LSTM_INT_E_OUT_OF_MEMORY;
       } else if (hipMemcpy(m->base, img.data(), img.size(), hipMemcpyHostToDevice) != hipSuccess) {
         rc = LSTM_INT_E_DEVICE;

@@ -215,6 +215,27 @@ def test_sums_of_decay_are_taken_where_they_matter():
     check(y, new, reference(q, k, v, g, beta, state), 64, 64 ** -0.5)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("by", [1e-25, 1e-6, 1e6, 1e25])
+def test_magnitudes(by, dtype):
+    # states and values far from one, columns far from each other, and a state far from what is written to it
+    q, k, v, g, beta, state = make(100, 1, 1, 2, 64, 48, dtype, seed=13)
+    columns = 10.0 ** torch.linspace(-5, 5, 48)
+    v, state = (v.float() * by * columns).to(dtype), state * by * columns
+    state[:, 1] *= 1e-6
+    y, new = run((q, k, v, g, beta, state))
+    want = reference(q, k, v, g, beta, state)
+    for c in range(48):  # the bound of check(), for each column by itself
+        s = float(columns[c]) * by
+        part = [want[0][..., c:c + 1] / s, want[1][..., c:c + 1] / s]
+        most = max(1.0, np.sqrt((part[1] ** 2).sum((2, 3))).max(), float((v[..., c].double() / s).abs().max()), float(state[..., c].norm(dim=2).max() / s))
+        walk = 4 * 101 ** 0.5 * 16 * 2.0 ** -24 * most
+        assert np.abs(new[..., c].double().cpu().numpy() / s - part[1][..., 0]).max() <= walk
+        off = np.abs(y[..., c].double().cpu().numpy() / s - part[0][..., 0])
+        f = torch.finfo(dtype)
+        assert (off <= walk * 64 ** -0.5 + np.abs(part[0][..., 0]) * f.eps / 2 + f.smallest_normal * f.eps / s).all()
+
+
 def test_values_that_are_not_finite_stay_in_their_head_and_row():
     T = 100
     args = make(T, 2, 2, 2, 64, 32, BF16, seed=11)

@@ -83,6 +83,18 @@ def test_strided_rows_and_neighbours(M):
     assert (out[:, :11] == -5).all() and (out[:, 88:] == -5).all()
 
 
+@pytest.mark.parametrize("M, K", [(65536 * 64 + 5, 20), (65536 * 128 + 3, 130)])
+def test_more_rows_than_a_grid_dimension_has(M, K):
+    codes, scales, x, _, _ = make(997, K, 18, 32, seed=3)
+    m = binding.w4_prepare(codes=codes, scales=scales, group=32)
+    y = m.forward(torch.from_numpy(x).cuda().repeat(-(-M // 997), 1)[:M], 0.1)
+    once = m.forward(torch.from_numpy(x).cuda(), 0.1)
+    check(once, codes, scales, 32, x, 0.1)
+    for at in (0, 997 * 500, M // 997 * 997 - 997):
+        assert torch.equal(y[at:at + 997], once)
+    assert torch.equal(y[M // 997 * 997:], once[:M % 997])
+
+
 def test_leading_dimensions_an_empty_batch_and_refusals():
     codes, scales, x, a, _ = make(12, 64, 20, 32)
     m = binding.w4_prepare(codes=codes, scales=scales, group=32)

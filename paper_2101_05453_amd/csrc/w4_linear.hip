@@ -165,7 +165,7 @@ __device__ inline void w4_store(const W4Args &a, f32x4 acc, float am, f32x4 bias
 // the first is used; the parts of a tile meet in LDS, in the order of the waves.
 template <int kGroup, int kRows, bool kZero, class T>
 __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
-  constexpr int kAhead = kRows == 4 ? 2 : 4, per_chunk = kChunk / kGroup;
+  constexpr int kAhead = kRows == 4 || kGroup == 32 ? 2 : 4, per_chunk = kChunk / kGroup;
   __shared__ f32x4 part[8][kRows][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tile = blockIdx.x % a.across * (8 / a.split) + wave / a.split, p = wave % a.split;
@@ -221,10 +221,21 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
 template <int kGroup, bool kZero, class T>
 __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   constexpr int per_chunk = kChunk / kGroup;
-  __shared__ u32x4 xs[2][8][2][64];  // [row tile][64 inputs][operand order]
-  __shared__ u32x4 ws[2][8][64];     // [output tile]
-  __shared__ f32x4 ss[2][8 * per_chunk * 4];
-  __shared__ u32x4 zs[2][8 * per_chunk * 2];
+  // results on their way out: rows of 128, a half of them at a time in float32, 16 bytes apart from multiples of all banks
+  constexpr int kOutRows = sizeof(T) == 4 ? 64 : 128, kOutLd = 128 + 16 / sizeof(T);
+  __shared__ union {
+    struct {
+      u32x4 xs[2][8][2][64];  // [row tile][64 inputs][operand order]
+      u32x4 ws[2][8][64];     // [output tile]
+      f32x4 ss[2][8 * per_chunk * 4];
+      u32x4 zs[2][8 * per_chunk * 2];
+    };
+    T out[kOutRows][kOutLd];
+  } lds;
+  auto &xs = lds.xs;
+  auto &ws = lds.ws;
+  auto &ss = lds.ss;
+  auto &zs = lds.zs;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, i16 = lane & 15;
   const int nb = blockIdx.x % a.across;
   const int64_t m0 = (int64_t)(blockIdx.x / a.across) * 128;
@@ -299,14 +310,38 @@ __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   f32x4 bias[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) bias[j] = bias_of(a, (tile0 + j) * kTile + 4 * kg);
+  // through LDS into whole rows: a lane's four outputs of each of 16 rows are pieces of 32 bytes in memory (16384 x 640 ->
+  // 8192: 192 us so, 166 as rows of 256 bytes)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + (mt0 + i) * 16 + i16;
-    const float am = row_scale(a, m);
-    if (m >= a.M) continue;
+  for (int half = 0; half < 128 / kOutRows; ++half) {
+    if (half) __syncthreads();
+    if (kOutRows == 128 || wave >> 2 == half)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (tile0 + j < a.tiles) w4_store<T>(a, acc[j][i], am, bias[j], m, (tile0 + j) * kTile + 4 * kg);
+      for (int i = 0; i < 4; ++i) {
+        const int m = (mt0 + i) * 16 + i16;
+        const float am = row_scale(a, m0 + m);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          T *to = &lds.out[m % kOutRows][(nt0 + j) * kTile + 4 * kg];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[r] = (T)(am * acc[j][i][r] + bias[j][r]);
+        }
+      }
+    __syncthreads();
+    constexpr int kPiece = 16 / sizeof(T), kPieces = 128 / kPiece;  // of a row
+#pragma unroll
+    for (int e = 0; e < kOutRows * kPieces / 512; ++e) {
+      const int id = e * 512 + tid, row = id / kPieces, at = id % kPieces * kPiece, n = nb * 128 + at;
+      const int64_t m = m0 + half * kOutRows + row;
+      if (m >= a.M || n >= a.N) continue;
+      T *y = static_cast<T *>(a.y) + m * a.y_stride + n;
+      const T *from = &lds.out[row][at];
+      if (n + kPiece <= a.N) *reinterpret_cast<u32x4_any *>(y) = *reinterpret_cast<const u32x4 *>(from);
+      else
+#pragma unroll
+        for (int r = 0; r < kPiece; ++r)
+          if (n + r < a.N) y[r] = from[r];
+    }
   }
 }
 

@@ -347,7 +347,11 @@ __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
 
 template <int kGroup, bool kZero, class T>
 int launch_w4(W4Args a, hipStream_t s) {
-  const bool blocks = a.M > 64 && a.chunks > 1;
+  // A chunk of blocks takes what some 900 pieces of 64 rows x 16 outputs take by themselves, spread over the device.  us, rows
+  // / blocks, at 900 and on both sides: 4096 inputs and outputs, 192 and 256 rows 30 / 33 and 39 / 33; 640 inputs, 8192
+  // outputs, 64 and 96 rows 6.1 / 7.1 and 9.5 / 7.6; 1024 and 1024, 512 rows 8.7 / 10.8; 512 and 32000, 32 rows 9.1 / 6.5;
+  // the same in groups of 32, where both take twice as long.
+  const bool blocks = a.M > 16 && a.chunks > 1 && (int64_t)((a.M + 63) / 64) * a.tiles > 900;
   const int rows = blocks ? 128 : a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64, tiles = blocks ? 8 : 8 / a.split;
   a.across = (a.tiles + tiles - 1) / tiles;
   const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536

@@ -34,7 +34,9 @@ def check(y, codes, scales, group, x, a, zp=0, bias=None):
 
 SIZES = [(1, 1, 1), (1, 128, 16), (1, 2048, 2048), (2, 75, 33), (3, 640, 1003), (7, 129, 17), (15, 1000, 100), (16, 256, 256), (17, 300, 65),
          (31, 96, 47), (33, 4096, 130), (64, 513, 200), (65, 128, 128), (100, 640, 77), (128, 384, 300), (129, 255, 129), (300, 200, 150),
-         (513, 1024, 260), (1000, 640, 512)]
+         (513, 1024, 260), (1000, 640, 512),
+         # enough rows and outputs for blocks of 128 x 128
+         (33, 513, 16003), (65, 384, 8200), (129, 255, 5003), (300, 1000, 3001), (1000, 200, 1000), (2049, 130, 470), (17, 129, 14500)]
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
@@ -60,6 +62,32 @@ def test_the_zero_point_is_exact(M, group):
         x = torch.full((M, 333), zp, dtype=torch.int8, device="cuda")
         y = binding.w4_prepare(codes=codes, scales=scales, group=group, bias=bias).forward(x, 0.7, zero_point=zp, dtype=torch.float32)
         assert torch.equal(y.cpu(), torch.from_numpy(bias).expand(M, 90))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_blocks_of_a_zero_point_of_strided_rows_and_captured(group):
+    M, K, N = 200, 333, 4003
+    codes, scales, x, a, bias = make(M, K, N, group, seed=11)
+    m = binding.w4_prepare(codes=codes, scales=scales, group=group, bias=bias)
+    for zp in (-128, 127):
+        y = m.forward(torch.full((M, K), zp, dtype=torch.int8, device="cuda"), 0.7, zero_point=zp, dtype=torch.float32)
+        assert torch.equal(y.cpu(), torch.from_numpy(bias).expand(M, N))
+    wide, out = torch.full((M, K + 9), 77, dtype=torch.int8, device="cuda"), torch.full((M, N + 5), -5.0, device="cuda")
+    wide[:, 4:K + 4] = torch.from_numpy(x).cuda()
+    ad, y = torch.from_numpy(a).cuda(), out[:, 2:N + 2]
+    m.forward(wide[:, 4:K + 4], ad, y=y)
+    check(y, codes, scales, group, x, a, bias=bias)
+    assert (out[:, :2] == -5).all() and (out[:, N + 2:] == -5).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.forward(wide[:, 4:K + 4], ad, y=y)
+    for k in range(3):
+        x2 = np.roll(x, k + 1, 1)
+        wide[:, 4:K + 4] = torch.from_numpy(x2).cuda()
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(y, codes, scales, group, x2, a, bias=bias)
 
 
 def test_quantized_here():

@@ -23,18 +23,20 @@ struct DeltaArgs {
 
 constexpr float kNormEps = 1e-6f;
 
-// Step by step: a wave has 16 columns of one head's state in registers, lane (r = lane / 4, c = lane % 4) the rows
-// kRows r .. kRows r + kRows - 1 of columns 4 c .. 4 c + 3.  S' k and S' q are taken of the state before the step, in one
-// reduction over the lanes, and y = e^g S' q + (k' q) u follows from them: a step waits for one reduction.
-template <class T, int kRows>
+// Step by step: a wave has 4 kLanes columns of one head's state in registers, lane (r = lane / kLanes, c = lane % kLanes)
+// the rows kRows r .. kRows r + kRows - 1 of columns 4 c .. 4 c + 3.  S' k and S' q are taken of the state before the step,
+// in one reduction over the lanes, and y = e^g S' q + (k' q) u follows from them: a step waits for one reduction.  A single
+// step is bound by the state's way in and out.
+template <class T, int kLanes, int kRows>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
+  constexpr int kColumns = 4 * kLanes;
   const int lane = threadIdx.x & 63;
-  const int tiles = (a.Dv + 15) / 16;
+  const int tiles = (a.Dv + kColumns - 1) / kColumns;
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (item >= (int64_t)a.B * a.Hv * tiles) return;
   const int tile = (int)(item % tiles), h = (int)(item / tiles % a.Hv), b = (int)(item / tiles / a.Hv);
   const int hk = h / (a.Hv / a.Hk);
-  const int r0 = (lane >> 2) * kRows, c0 = tile * 16 + (lane & 3) * 4;
+  const int r0 = lane / kLanes * kRows, c0 = tile * kColumns + lane % kLanes * 4;
   const int nr = max(0, min(kRows, a.Dk - r0)), nc = max(0, min(4, a.Dv - c0));
   const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
 
@@ -88,7 +90,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
       }
     }
 #pragma unroll
-    for (int m = 4; m < 64; m <<= 1) {
+    for (int m = kLanes; m < 64; m <<= 1) {
       kk += __shfl_xor(kk, m);
       qq += __shfl_xor(qq, m);
       kq += __shfl_xor(kq, m);
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) S[i][j] = __builtin_fmaf(nk * kf[i], u[j], decay * S[i][j]);
-    if (lane < 4)
+    if (lane < kLanes)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (j < nc) y[t * a.y_stride[0] + j] = (T)o[j];
@@ -127,12 +129,20 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a) {
     }
 }
 
+template <class T, int kLanes, int kRows>
+int launch_step(const DeltaArgs &a, hipStream_t s) {
+  const int64_t items = (int64_t)a.B * a.Hv * ((a.Dv + 4 * kLanes - 1) / (4 * kLanes));
+  return launch(delta_step_kernel<T, kLanes, kRows>, dim3((unsigned)((items + 3) / 4)), dim3(256), s, a);
+}
+
 template <class T>
 int launch_step(const DeltaArgs &a, hipStream_t s) {
-  const int64_t items = (int64_t)a.B * a.Hv * ((a.Dv + 15) / 16);
-  const dim3 grid((unsigned)((items + 3) / 4)), block(256);
-  return a.Dk <= 64 ? launch(delta_step_kernel<T, 4>, grid, block, s, a)
-                    : a.Dk <= 128 ? launch(delta_step_kernel<T, 8>, grid, block, s, a) : launch(delta_step_kernel<T, 16>, grid, block, s, a);
+  // 32 columns to a wave, whole lines of memory, where that leaves enough waves and registers: one step of 64 x 16 heads of
+  // 128 x 128 takes 37 us with 16 columns and 30 with 32, 4.5 TB/s of state
+  const bool wide = (int64_t)a.B * a.Hv * ((a.Dv + 31) / 32) >= 1024;
+  if (a.Dk <= 64) return wide ? launch_step<T, 8, 8>(a, s) : launch_step<T, 4, 4>(a, s);
+  if (a.Dk <= 128) return wide ? launch_step<T, 8, 16>(a, s) : launch_step<T, 4, 8>(a, s);
+  return launch_step<T, 4, 16>(a, s);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -141,14 +151,15 @@ int launch_step(const DeltaArgs &a, hipStream_t s) {
 //   u = X (v - diag(e^c) K S),   y = diag(e^c) Q S + P u,   P_ij = e^(c_i - c_j) q_i'k_j  (j <= i)
 //   S <- e^(c_last) S + K' diag(e^(c_last - c)) u
 // X and P do not depend on the state: delta_prep_kernel computes them for all chunks side by side.  delta_scan_kernel
-// carries the state from chunk to chunk.
+// carries the state from chunk to chunk.  One kernel for both would read K and Q once less, and would either repeat the first
+// part for each group of value columns or have it wait in front of every chunk.
 //
 // Products run on the fp16 MFMA, whose products are exact and whose sums are float32.  A float32 operand is scaled by a power
 // of two -- each row of a left operand and each column of a right one by its own -- and taken as two fp16 parts: 22 bits of
 // each element, and 2^-25 of the largest.  Of the products of parts the one of the two low ones, 2^-22 of the others, is
 // left out.  bf16 and fp16 keys and queries are one part.  So results are as exact as float32 products, at two or three
-// MFMAs for one, where the float32 MFMA takes 16 times the time (three bf16 parts, which need no scales, took three to
-// six, and twice the vector instructions for the parts of a state: 2048 steps of 8 x 32 heads 280 us for this kernel).
+// MFMAs for one, where the float32 MFMA takes 16 times the time.  (Three bf16 parts, which need no scales, took three to six,
+// and more vector instructions: 777 ragged steps of 5 x 6 float32 heads 141 us, 96 so.)
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kChunk = 32;
 constexpr int kHeadsOfGrid = 1 << 15;  // blockIdx.y of the first kernel, blockIdx.z counts on
@@ -271,7 +282,7 @@ __device__ inline void place(Raw4<T> (&rows)[kN], int col, int width) {
 struct ChunkArgs {
   DeltaArgs d;
   uint32_t *items;  // [B Hv][chunks][kItemWords]
-  int chunks;
+  int chunks, heads;  // heads: value heads that a wave of the first kernel prepares, all of one key head
 };
 
 __device__ inline int length_of(const DeltaArgs &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
@@ -311,7 +322,8 @@ struct Inputs {
   }
 };
 
-// One wave per chunk and value head: X, P and the factors of its steps
+// One wave per chunk and value head, or all of a key head's: X, P and the factors of its steps.  Vector instructions and
+// the chain of the substitution bound it: 64 chunks of 8 x 16 key heads of 128, two value heads each, 87 us.
 template <class T, int kDk, bool kWhole>  // kWhole: key_dim = kDk
 __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
   constexpr int kLd = 36, kBlocks = kDk / 32;
@@ -321,23 +333,12 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
   __shared__ float rate[kChunk], norm_k[kChunk], norm_q[kChunk];
   const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
   const int chunk = blockIdx.x;
-  const int bh = blockIdx.z * kHeadsOfGrid + blockIdx.y;
-  if (bh >= d.B * d.Hv) return;
-  const int b = bh / d.Hv, h = bh % d.Hv, hk = h / (d.Hv / d.Hk);
+  const int item_at = blockIdx.z * kHeadsOfGrid + blockIdx.y;  // of B Hv / heads
+  const int bh0 = item_at * a.heads;
+  if (bh0 >= d.B * d.Hv) return;
+  const int b = bh0 / d.Hv, hk = bh0 % d.Hv / (d.Hv / d.Hk);
   const int t0 = chunk * kChunk, left = length_of(d, b) - t0;  // steps of the row from here on
   if (left <= 0) return;
-  uint32_t *item = a.items + ((int64_t)bh * a.chunks + chunk) * kItemWords;
-  float *factors = reinterpret_cast<float *>(item + 2 * kMatrix);
-  double c = 0;
-  float bt = 0;
-  {
-    const int t = lane & 31;
-    if (t < left) {
-      const float gv = d.g[b * d.g_stride[1] + h * d.g_stride[2] + (int64_t)(t0 + t) * d.g_stride[0]];
-      c = gv < -1000.0f ? -1000.0 : (double)gv;  // e^-1000 is zero; the sum stays a number
-      bt = d.beta[b * d.beta_stride[1] + h * d.beta_stride[2] + (int64_t)(t0 + t) * d.beta_stride[0]];
-    }
-  }
   // rows behind the last step are that step again: their rate of writing is zero
   const T *kp = static_cast<const T *>(d.k) + b * d.k_stride[1] + hk * d.k_stride[2];
   const T *qp = static_cast<const T *>(d.q) + b * d.q_stride[1] + hk * d.q_stride[2];
@@ -392,16 +393,7 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
       qk[2] = Inputs<T>::product(qf[1], kf[1], qk[2]);
     }
   }
-#pragma unroll
-  for (int m = 1; m < 32; m <<= 1) {
-    union { double v; int w[2]; } x, y;
-    x.v = c;
-    y.w[0] = __shfl_up(x.w[0], m, 32);
-    y.w[1] = __shfl_up(x.w[1], m, 32);
-    if ((lane & 31) >= m) c += y.v;
-  }
-  if (lane < 32) sum_g[lane] = c, rate[lane] = bt;
-  float inv_sk[2], inv_sq[2];
+  float inv_sk[2], inv_sq[2], up_k[2], up_q[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     sk[m] += __shfl_xor(sk[m], 16);
@@ -413,98 +405,139 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
     if (g == 0) {
       norm_k[16 * m + i] = d.normalize ? 1.0f / sqrtf(sk[m] + kNormEps) : 1.0f;
       norm_q[16 * m + i] = (d.normalize ? 1.0f / sqrtf(sq[m] + kNormEps) : 1.0f) * d.scale;
-      factors[kSk * kChunk + 16 * m + i] = ks.up;
-      factors[kSq * kChunk + 16 * m + i] = qs.up;
     }
+    up_k[m] = ks.up, up_q[m] = qs.up;
   }
-  __syncthreads();
-  if (g < 2) {  // lane = step
-    const double end = sum_g[kChunk - 1];
-    const float e = expf((float)c), dk = g ? inv_sk[1] : inv_sk[0], dq = g ? inv_sq[1] : inv_sq[0];
-    factors[kFk * kChunk + lane] = e * norm_k[lane] * dk;
-    factors[kFq * kChunk + lane] = e * norm_q[lane] * dq;
-    factors[kFu * kChunk + lane] = expf((float)(end - c)) * norm_k[lane] * dk;
-    factors[kFwhole * kChunk + lane] = expf((float)end);
-  }
-#pragma unroll
-  for (int tile = 0; tile < 3; ++tile) {
-    const int tj = (tile == 2 ? 16 : 0) + i;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int ti = (tile ? 16 : 0) + 4 * g + r;
-      const float e = ti >= tj ? expf((float)(sum_g[ti] - sum_g[tj])) * norm_k[tj] : 0.0f;
-      mat[0][ti * kLd + tj] = ti > tj ? e * kk[tile][r] * norm_k[ti] * rate[ti] : 0.0f;
-      mat[1][ti * kLd + tj] = ti >= tj ? e * qk[tile][r] * norm_q[ti] : 0.0f;
+  // what follows differs from value head to value head
+#pragma unroll 1
+  for (int n = 0; n < a.heads; ++n) {
+    // the lane again, from nothing: places in LDS that are computed ahead of the loop would take half of the registers
+    int lane = threadIdx.x;
+    asm volatile("" : "+v"(lane));
+    const int i = lane & 15, g = lane >> 4;
+    const int bh = bh0 + n, h = bh % d.Hv;
+    uint32_t *item = a.items + ((int64_t)bh * a.chunks + chunk) * kItemWords;
+    float *factors = reinterpret_cast<float *>(item + 2 * kMatrix);
+    double c = 0;
+    float bt = 0;
+    if ((lane & 31) < left) {
+      const int64_t t = t0 + (lane & 31);
+      const float gv = d.g[b * d.g_stride[1] + h * d.g_stride[2] + t * d.g_stride[0]];
+      c = gv < -1000.0f ? -1000.0 : (double)gv;  // e^-1000 is zero; the sum stays a number
+      bt = d.beta[b * d.beta_stride[1] + h * d.beta_stride[2] + t * d.beta_stride[0]];
     }
-  }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) mat[1][(4 * g + r) * kLd + 16 + i] = 0;
-  __syncthreads();
-  // (1 + A)^-1: the 16 x 16 blocks on the diagonal by substitution, a lane a column; then the one below them
-  {
-    const int blk = g & 1;
-    const float *A = mat[0] + 16 * blk * (kLd + 1);
-    float x[16];
+    for (int m = 1; m < 32; m <<= 1) {
+      union { double v; int w[2]; } x, y;
+      x.v = c;
+      y.w[0] = __shfl_up(x.w[0], m, 32);
+      y.w[1] = __shfl_up(x.w[1], m, 32);
+      if ((lane & 31) >= m) c += y.v;
+    }
+    if (lane < 32) sum_g[lane] = c, rate[lane] = bt;
+    if (g == 0)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float s0 = r == i ? 1.0f : 0.0f, s1 = 0;
-#pragma unroll
-      for (int m = 0; m < r; m += 4) {
-        const f32x4 row = *reinterpret_cast<const f32x4 *>(A + r * kLd + m);
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-          if (m + n < r) (n % 2 ? s1 : s0) = __builtin_fmaf(-row[n], x[m + n], n % 2 ? s1 : s0);
+      for (int m = 0; m < 2; ++m) {
+        factors[kSk * kChunk + 16 * m + i] = up_k[m];
+        factors[kSq * kChunk + 16 * m + i] = up_q[m];
       }
-      x[r] = s0 + s1;
-      if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // rows of A are read a few ahead, not all at once
+    __syncthreads();
+    if (g < 2) {  // lane = step
+      const double end = sum_g[kChunk - 1];
+      const float e = expf((float)c), dk = g ? inv_sk[1] : inv_sk[0], dq = g ? inv_sq[1] : inv_sq[0];
+      factors[kFk * kChunk + lane] = e * norm_k[lane] * dk;
+      factors[kFq * kChunk + lane] = e * norm_q[lane] * dq;
+      factors[kFu * kChunk + lane] = expf((float)(end - c)) * norm_k[lane] * dk;
+      factors[kFwhole * kChunk + lane] = expf((float)end);
+    }
+#pragma unroll
+    for (int tile = 0; tile < 3; ++tile) {
+      const int tj = (tile == 2 ? 16 : 0) + i;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int ti = (tile ? 16 : 0) + 4 * g + r;
+        const float e = ti >= tj ? expf((float)(sum_g[ti] - sum_g[tj])) * norm_k[tj] : 0.0f;
+        mat[0][ti * kLd + tj] = ti > tj ? e * kk[tile][r] * norm_k[ti] * rate[ti] : 0.0f;
+        mat[1][ti * kLd + tj] = ti >= tj ? e * qk[tile][r] * norm_q[ti] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mat[1][(4 * g + r) * kLd + 16 + i] = 0;
+    __syncthreads();
+    // (1 + A)^-1: the 16 x 16 blocks on the diagonal by substitution, a lane a column; then the one below them
+    {
+      const int blk = g & 1;
+      const float *A = mat[0] + 16 * blk * (kLd + 1);
+      float x[16];
+      int from = 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float s0 = r == i ? 1.0f : 0.0f, s1 = 0;
+#pragma unroll
+        for (int m = 0; m < r; m += 4) {
+          const f32x4 row = *reinterpret_cast<const f32x4 *>(A + from + r * kLd + m);
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            if (m + n < r) (n % 2 ? s1 : s0) = __builtin_fmaf(-row[n], x[m + n], n % 2 ? s1 : s0);
+        }
+        x[r] = s0 + s1;
+        // the next four rows of A are read behind this one, not all sixteen at once: half of the registers
+        if (r % 4 == 3) asm volatile("" : "+v"(from), "+v"(x[r]));
+      }
+      __syncthreads();
+      if (g < 2)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mat[0][(16 * blk + r) * kLd + 16 * blk + i] = x[r];
     }
     __syncthreads();
-    if (g < 2)
+    {
+      f32x4 m1 = {0, 0, 0, 0}, m2 = {0, 0, 0, 0};
+      const f32x4 below = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 4 * g]);
+      const f32x4 last = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 16 + 4 * g]);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mat[0][(16 * blk + r) * kLd + 16 * blk + i] = x[r];
-  }
-  __syncthreads();
-  {
-    f32x4 m1 = {0, 0, 0, 0}, m2 = {0, 0, 0, 0};
-    const f32x4 below = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 4 * g]);
-    const f32x4 last = *reinterpret_cast<const f32x4 *>(&mat[0][(16 + i) * kLd + 16 + 4 * g]);
+      for (int r = 0; r < 4; ++r) m1 = __builtin_amdgcn_mfma_f32_16x16x4f32(below[r], mat[0][(4 * g + r) * kLd + i], m1, 0, 0, 0);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) m1 = __builtin_amdgcn_mfma_f32_16x16x4f32(below[r], mat[0][(4 * g + r) * kLd + i], m1, 0, 0, 0);
+      for (int r = 0; r < 4; ++r) m2 = __builtin_amdgcn_mfma_f32_16x16x4f32(last[r], m1[r], m2, 0, 0, 0);
+      __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 4; ++r) m2 = __builtin_amdgcn_mfma_f32_16x16x4f32(last[r], m1[r], m2, 0, 0, 0);
+      for (int r = 0; r < 4; ++r) {
+        mat[0][(16 + 4 * g + r) * kLd + i] = -m2[r];
+        mat[0][(4 * g + r) * kLd + 16 + i] = 0;
+      }
+    }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      mat[0][(16 + 4 * g + r) * kLd + i] = -m2[r];
-      mat[0][(4 * g + r) * kLd + 16 + i] = 0;
-    }
-  }
-  __syncthreads();
+    for (int w = 0; w < 2; ++w)
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
+      for (int m = 0; m < 2; ++m) {
+        f32x4 v[2];
+        uint32_t most = 0;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      f32x4 v[2];
-      uint32_t most = 0;
+        for (int e = 0; e < 2; ++e) {
+          v[e] = *reinterpret_cast<const f32x4 *>(&mat[w][(16 * m + i) * kLd + 16 * e + 4 * g]);
+          if (w == 0) v[e] *= *reinterpret_cast<const f32x4 *>(&rate[16 * e + 4 * g]);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        v[e] = *reinterpret_cast<const f32x4 *>(&mat[w][(16 * m + i) * kLd + 16 * e + 4 * g]);
-        if (w == 0) v[e] *= *reinterpret_cast<const f32x4 *>(&rate[16 * e + 4 * g]);
+          for (int j = 0; j < 4; ++j) most = max(most, bits_of(v[e][j]));
+        }
+        const Scale s = scale_of(over_column(most));  // lanes i, i + 16, ...: the row's
+        Frag f[2];
+        split8(v[0] * s.up, v[1] * s.up, f, minus_one());
 #pragma unroll
-        for (int j = 0; j < 4; ++j) most = max(most, bits_of(v[e][j]));
+        for (int p = 0; p < 2; ++p) *reinterpret_cast<u32x4 *>(item + w * kMatrix + ((m * 2 + p) * 64 + lane) * 4) = f[p].w;
+        if (g == 0) factors[(w ? kFp : kFx) * kChunk + 16 * m + i] = s.down;
       }
-      const Scale s = scale_of(over_column(most));  // lanes i, i + 16, ...: the row's
-      Frag f[2];
-      split8(v[0] * s.up, v[1] * s.up, f, minus_one());
-#pragma unroll
-      for (int p = 0; p < 2; ++p) *reinterpret_cast<u32x4 *>(item + w * kMatrix + ((m * 2 + p) * 64 + lane) * 4) = f[p].w;
-      if (g == 0) factors[(w ? kFp : kFx) * kChunk + 16 * m + i] = s.down;
-    }
+    __syncthreads();  // mat and the sums are the next head's
+  }
 }
 
 // A workgroup carries kMain * kCols * 16 columns of one head's state through the sequence: kMain waves have 16 kCols columns
 // each, in the registers, for good; four more ("loaders") bring the next chunk's operands into LDS meanwhile, in parts and
 // in the MFMA's order, with the chunk after it already requested.  kBuffers = 1 where two do not fit.
+//
+// With a workgroup on each compute unit it is bound by the issue of vector instructions: 1060 to a SIMD and chunk (parts of
+// the state and their scales, the loaders' transposition), 51 % of all cycles, 68 % with the others; LDS 24 %, MFMA 23 %.
+// 2048 steps of 8 x 32 heads of 128 x 128: 250 us, 3.9 us a chunk.  With fewer it is bound by the chain of a chunk, K S ->
+// u -> S: 1.6 us for 32 steps.
 template <class T, int kDk, int kMain, int kCols>
 struct Scan {
   static constexpr int kP = kParts<T>, kBlocks = kDk / 32, kLoaders = 4, kColumns = 16 * kMain * kCols;
@@ -906,7 +939,9 @@ int launch_scan(const ChunkArgs &a, hipStream_t s) {
   return launch(delta_scan_kernel<T, kDk, kMain, kCols>, grid, dim3((kMain + 4) * 64), s, a);
 }
 
-// As many columns to a workgroup as leave one for each compute unit: their operands come from memory once
+// As many columns to a workgroup as leave one for each compute unit: their operands come from memory once.  (2048 steps of
+// 8 x 32 heads, 128 columns in four waves of 32, in eight waves of 16, 64 columns in four of 16: 373, 382, 443 us; float32
+// 511, 612, 627.)
 template <class T, int kDk>
 int launch_scan(const ChunkArgs &a, hipStream_t s) {
   const int64_t heads = (int64_t)a.d.B * a.d.Hv;
@@ -924,8 +959,8 @@ int launch_scan(const ChunkArgs &a, hipStream_t s) {
 
 template <class T, int kDk>
 int launch_chunks(const ChunkArgs &a, hipStream_t s) {
-  const int heads = a.d.B * a.d.Hv;
-  const dim3 grid(a.chunks, std::min(heads, kHeadsOfGrid), (heads + kHeadsOfGrid - 1) / kHeadsOfGrid);
+  const int items = a.d.B * a.d.Hv / a.heads;
+  const dim3 grid(a.chunks, std::min(items, kHeadsOfGrid), (items + kHeadsOfGrid - 1) / kHeadsOfGrid);
   const int rc = a.d.Dk == kDk ? launch(delta_prep_kernel<T, kDk, true>, grid, dim3(64), s, a)
                                : launch(delta_prep_kernel<T, kDk, false>, grid, dim3(64), s, a);
   return rc != LSTM_INT_OK ? rc : launch_scan<T, kDk>(a, s);
@@ -983,7 +1018,11 @@ int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, 
   if (!scope.ok) return LSTM_INT_E_DEVICE;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   if (in_chunks(p)) {
-    const ChunkArgs c{a, static_cast<uint32_t *>(workspace), (p->steps + kChunk - 1) / kChunk};
+    ChunkArgs c{a, static_cast<uint32_t *>(workspace), (p->steps + kChunk - 1) / kChunk, 1};
+    // The products of keys and queries are the same for all value heads of a key head: a wave for all of them, as long as
+    // that leaves the device full.  2048 steps, two value heads to each of 8 x 16 key heads 379 us instead of 400, of 4 x 16
+    // 183 instead of 191; four to each of 8 x 8 311 instead of 342.
+    if ((int64_t)p->batch * p->key_heads * c.chunks >= 4096) c.heads = p->value_heads / p->key_heads;
     return p->dtype == LM_F32 ? launch_chunks<float>(c, s) : p->dtype == LM_F16 ? launch_chunks<_Float16>(c, s) : launch_chunks<__bf16>(c, s);
   }
   return p->dtype == LM_F32 ? launch_step<float>(a, s) : p->dtype == LM_F16 ? launch_step<_Float16>(a, s) : launch_step<__bf16>(a, s);

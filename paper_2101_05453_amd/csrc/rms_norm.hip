@@ -6,7 +6,12 @@
 // per lane and slot, as it lies in memory, from its load to the store of its codes.  A code at the border between two has
 // to be the definition's, so sums of squares are double precision and n is evaluated twice: in float32 for every element,
 // and in double precision for the few that this leaves open -- the row's largest, which the scale is made of, and those
-// whose n / s comes out within 2^-12 of a border.
+// whose n / s comes out within its rounding of a border.  (In double precision throughout, 8192 x 4096 in heads of 128 with a
+// gate took 129 us.)
+//
+// Bound by memory where it is large and plain: 8192 x 4096 bf16 with a residual 52 us, 4.5 TB/s; by vector instructions with
+// a gate, 36 an element: the same in heads of 128, 71 us, 2.3 TB/s; by the chain load, sum, largest, store where it is small:
+// one row of 2048 5 us.
 #include "lm_common.h"
 
 namespace lstm_int {

@@ -74,7 +74,9 @@ def run(args, normalize=True, **kw):
 SIZES = [(1, 1, 1, 1, 128, 128), (1, 3, 2, 4, 64, 64), (1, 2, 1, 1, 1, 1), (2, 1, 1, 3, 17, 33), (5, 2, 2, 2, 128, 80), (15, 1, 1, 2, 96, 16),
          (16, 1, 1, 1, 128, 128), (33, 2, 1, 2, 100, 50), (63, 1, 2, 2, 64, 64), (64, 1, 1, 1, 128, 128), (65, 2, 1, 2, 128, 96),
          (127, 1, 1, 1, 75, 130), (128, 2, 2, 4, 32, 17), (130, 1, 1, 2, 256, 64), (200, 3, 2, 2, 128, 128), (257, 1, 1, 1, 200, 256),
-         (300, 1, 3, 6, 16, 48), (500, 1, 1, 1, 7, 5)]
+         (300, 1, 3, 6, 16, 48), (500, 1, 1, 1, 7, 5),
+         # single steps of many heads; many chunks whose value heads share a key head
+         (1, 130, 4, 8, 128, 40), (3, 70, 2, 16, 33, 50), (70, 350, 4, 12, 32, 16), (130, 211, 4, 4, 20, 12)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16, FP32])

@@ -8,6 +8,7 @@
 // and exact, and begins with what the zero point takes off.
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <vector>
 
@@ -18,16 +19,18 @@ namespace {
 
 constexpr int kTile = 16, kChunk = 128;  // outputs and inputs of one 1 KB piece of weights
 
-// where weight (n, k) lies: piece (n / 16, k / 128); byte and nibble within it
-struct W4Place {
-  int byte;
-  bool high;
-};
-W4Place w4_place(int n, int k, int group) {
-  const int depth = group == 32 ? 32 : 64;  // inputs of one MFMA, which never spans two groups
-  const int kk = k % kChunk, j = kk / depth, in = kk % depth, per_lane = depth / 4;
-  const int lane = in / per_lane * 16 + n % kTile, e = in % per_lane;
-  return {lane * 16 + j / 2 * 8 + e, j % 2 == 0};
+// The 128 codes q of one output and chunk to their places in the piece of the output's tile.  Lane (n % 16, kg) has 16 bytes; a
+// byte's high nibble is of one product, the low one of the next: inputs 16 kg + e of 64 each, or, in groups of 32, inputs
+// 8 kg + e of 32 each, two products after the other (an MFMA never spans two groups).
+void w4_pack(const int8_t q[kChunk], int n, int group, uint8_t *piece) {
+  const int depth = group == 32 ? 32 : 64, per_lane = depth / 4;
+  for (int kg = 0; kg < 4; ++kg) {
+    uint8_t *to = piece + (kg * 16 + n % kTile) * 16;
+    for (int j = 0; j < kChunk / depth; j += 2) {
+      const int8_t *high = q + j * depth + kg * per_lane, *low = high + depth;
+      for (int e = 0; e < per_lane; ++e) to[j / 2 * per_lane + e] = (uint8_t)((uint8_t)high[e] << 4 | (low[e] & 15));
+    }
+  }
 }
 
 struct W4Args {
@@ -356,8 +359,12 @@ int launch_w4(W4Args a, hipStream_t s) {
   // outputs, 64 and 96 rows 6.1 / 7.1 and 9.5 / 7.6; 1024 and 1024, 512 rows 8.7 / 10.8; 512 and 32000, 32 rows 9.1 / 6.5;
   // the same in groups of 32, where both take twice as long.
   const bool blocks = a.M > 16 && a.chunks > 1 && (int64_t)((a.M + 63) / 64) * a.tiles > 900;
-  const int rows = blocks ? 128 : a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64, tiles = blocks ? 8 : 8 / a.split;
+  int rows = blocks ? 128 : a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
+  const int tiles = blocks ? 8 : 8 / a.split;
   a.across = (a.tiles + tiles - 1) / tiles;
+  // fewer rows to a wave where that takes a workgroup to more of the compute units: 1821 x
+  // 6592 -> 64 29 us in 64s, 17 so; 64 x 1024 -> 1024 5.3 and 3.3
+  while (!blocks && rows > 16 && (int64_t)a.across * ((a.M + rows - 1) / rows) < 256) rows /= 2;
   const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536
   if (count >= (int64_t)1 << 31) return LSTM_INT_E_UNSUPPORTED;
   const dim3 grid((unsigned)count), block(512);
@@ -453,22 +460,18 @@ int w4_linear_prepare(const w4_linear_params *p, int32_t device, w4_linear_model
       std::vector<uint8_t> img(m->o_bias + (m->bias ? tiles * kTile * 4 : 0), 0);
       float *s = reinterpret_cast<float *>(img.data() + m->o_s);
       int16_t *sums = reinterpret_cast<int16_t *>(img.data() + m->o_sums);
-      std::vector<W4Place> place((size_t)kTile * kChunk);
-      for (int n = 0; n < kTile; ++n)
-        for (int k = 0; k < kChunk; ++k) place[n * kChunk + k] = w4_place(n, k, G);
       for (int n = 0; n < N; ++n) {
         const size_t tile = n / kTile;
-        const W4Place *pl = &place[(size_t)(n % kTile) * kChunk];
-        for (int g = 0; g < groups; ++g) {
-          int sum = 0;
-          for (int k = g * G; k < std::min(K, (g + 1) * G); ++k) {
-            const int q = m->codes[(size_t)n * K + k];
-            const W4Place w = pl[k % kChunk];
-            img[(tile * m->chunks + k / kChunk) * 1024 + w.byte] |= (uint8_t)((q & 15) << (w.high ? 4 : 0));
-            sum += q;
+        for (int c = 0; c < m->chunks; ++c) {
+          int8_t q[kChunk] = {};
+          std::memcpy(q, &m->codes[(size_t)n * K + (size_t)c * kChunk], std::min(kChunk, K - c * kChunk));
+          w4_pack(q, n, G, img.data() + (tile * m->chunks + c) * 1024);
+          for (int g = c * (kChunk / G), i = 0; i < kChunk; ++g, i += G) {
+            int sum = 0;
+            for (int e = 0; e < G; ++e) sum += q[i + e];
+            sums[tile * per_tile + (size_t)g * kTile + n % kTile] = (int16_t)(16 * sum);
+            if (g < groups) s[tile * per_tile + (size_t)g * kTile + n % kTile] = m->scales[(size_t)n * groups + g] / 16;
           }
-          s[tile * per_tile + (size_t)g * kTile + n % kTile] = m->scales[(size_t)n * groups + g] / 16;
-          sums[tile * per_tile + (size_t)g * kTile + n % kTile] = (int16_t)(16 * sum);
         }
         if (m->bias) reinterpret_cast<float *>(img.data() + m->o_bias)[n] = p->bias[n];
       }

@@ -16,8 +16,9 @@
  * code, and no exception crosses this boundary.  `device` is the HIP device
  * that the pointers belong to; the calling thread's current device is left as
  * it was.  The online calls allocate nothing, never synchronize the host and
- * launch kernels only, so they can be captured in a HIP graph; a call that
- * returns an error has enqueued nothing.  Calls share no memory but what the
+ * launch kernels only, so that a caller may capture them in a HIP graph once one
+ * such call has run outside a capture; a call that returns an error has enqueued
+ * nothing that writes beyond its workspace.  Calls share no memory but what the
  * caller passes, so calls with different outputs (and workspaces) may overlap.
  * Unless it says "may be", an output overlaps no other argument.
  * There are no gradients: the library runs trained models.

@@ -362,8 +362,8 @@ int launch_w4(W4Args a, hipStream_t s) {
   int rows = blocks ? 128 : a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
   const int tiles = blocks ? 8 : 8 / a.split;
   a.across = (a.tiles + tiles - 1) / tiles;
-  // fewer rows to a wave where that takes a workgroup to more of the compute units: 1821 x
-  // 6592 -> 64 29 us in 64s, 17 so; 64 x 1024 -> 1024 5.3 and 3.3
+  // fewer rows to a wave where that takes a workgroup to more of the compute units: 1821 x 6592 -> 64 29 us in 64s, 17 so;
+  // 64 x 1024 -> 1024 5.3 and 3.3
   while (!blocks && rows > 16 && (int64_t)a.across * ((a.M + rows - 1) / rows) < 256) rows /= 2;
   const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536
   if (count >= (int64_t)1 << 31) return LSTM_INT_E_UNSUPPORTED;

@@ -321,7 +321,8 @@ int launch_norm(const NormArgs &a, hipStream_t s) {
 
 template <class T, int kWaves>
 int launch_norm(const NormArgs &a, hipStream_t s) {
-  return a.slots == 1 ? launch_norm<T, kWaves, 1>(a, s) : a.slots == 2 ? launch_norm<T, kWaves, 2>(a, s) : launch_norm<T, kWaves, kMostSlots>(a, s);
+  return a.slots == 1 ? launch_norm<T, kWaves, 1>(a, s) : a.slots == 2 || kWaves == 1 ? launch_norm<T, kWaves, 2>(a, s)
+                      : launch_norm<T, kWaves, kWaves == 1 ? 2 : kMostSlots>(a, s);
 }
 
 template <class T>
@@ -368,11 +369,15 @@ extern "C" int rms_norm_forward(int32_t device, const rms_norm_args *p, const vo
   while (a.lanes < 64 && a.lanes < chunks) a.lanes *= 2;
   a.per_group = (chunks + a.lanes - 1) / a.lanes;
   int waves = 1;
-  while (waves < 16 && slots_of(a, waves) > kMostSlots) waves *= 4;
-  // few rows: more waves for each, as long as they shorten it
+  // As few waves to a row as hold it.  One wave alone takes two slots at most: with four of them, and half as many waves on a
+  // compute unit, 1500 and 4096 bf16 rows of 2048 take 25 and 31 us, as four waves of a slot 11 and 21 (16384 rows 66, 65).
+  // Four waves do better than 16 at four slots too: 4096 and 16384 rows of 8192 65 and 240 us, by 16 waves 73 and 296.
+  while (waves < 16 && slots_of(a, waves) > (waves == 1 ? 2 : kMostSlots)) waves *= 4;
+  // Few rows: more waves for each, as long as they shorten it.  64 rows of 1024 7.0 us by one wave, 5.7 by four, 64 of 4096 7.3
+  // by four, 6.7 by 16; 272 rows of 4096 8.0 by four, 10.0 by 16; 4096 rows of 1024 11.8 by one, 17.7 by four.
   while (waves < 16 && a.rows * (int64_t)waves < 1024 && slots_of(a, waves) > 1) waves *= 4;
   a.slots = slots_of(a, waves);
-  a.row_lanes = a.groups == 1 && waves == 1 && a.slots == 1 ? a.lanes : 64;  // short rows: several to a wave
+  a.row_lanes = a.groups == 1 && waves == 1 && a.slots == 1 ? a.lanes : 64;  // short rows: several to a wave (65536 x 128: 18 us, one to a wave 59)
   if (a.slots > kMostSlots) return LSTM_INT_E_UNSUPPORTED;
 
   const DeviceScope scope(device);

@@ -170,6 +170,8 @@ __device__ inline void w4_store(const W4Args &a, f32x4 acc, float am, f32x4 bias
 // (1 x 2048 -> 2048 3.1 us, 32 x 4096 -> 4096 7.9).
 template <int kGroup, int kRows, bool kZero, class T>
 __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
+  // four chunks ahead where registers allow: 1 x 4096 -> 64000 35.0 us, two ahead 37.1; else two: 7 x 640 -> 32003 in groups of
+  // 32 8.2 us, four ahead 10.2, 128 x 4096 -> 4096 20.9 and 22.4
   constexpr int kAhead = kRows == 4 || kGroup == 32 ? 2 : 4, per_chunk = kChunk / kGroup;
   __shared__ f32x4 part[8][kRows][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -223,8 +225,8 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
 
 // Many rows: a workgroup of eight waves has 128 rows x 128 outputs, a wave 64 x 32 of them.  A chunk's operands and scales
 // go through LDS, two chunks deep.  Needs two chunks or more.  Bound by the latency of a chunk's loads and the stores, with 16
-// waves on a compute unit: 16384 x 640 -> 8192 166 us, 1.0 POP/s, of which 150 without the stores and as much without the
-// products; 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight needs registers that are not there (two stages: 295 us).
+// waves on a compute unit: 16384 x 640 -> 8192 166 us, 1.0 POP/s (at 192, before the stores went
+// through LDS, it was 150 without them, 177 without the products); 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight needs registers that are not there (two stages: 295 us).
 template <int kGroup, bool kZero, class T>
 __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   constexpr int per_chunk = kChunk / kGroup;

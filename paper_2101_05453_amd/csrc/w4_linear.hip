@@ -522,7 +522,9 @@ int w4_linear_forward(const w4_linear_model *m, const int8_t *x, int64_t x_strid
   a.M = (int)rows; a.N = m->N; a.K = m->K; a.tiles = (m->N + kTile - 1) / kTile; a.chunks = m->chunks; a.groups = m->dev_groups;
   a.zero_point = zero_point; a.scale = scale;
   a.split = 1;
-  while (a.split < 8 && a.split * 2 <= a.chunks && (int64_t)a.tiles * a.split < 2048) a.split *= 2;
+  // Waves share a tile's inputs until there are six to a compute unit.  One row of 4096 inputs, us: 8192 outputs by four waves
+  // 6.2, by two 9.5; 16384 by two 10.4, by one 16.2; 28000 by two 18.7, by one 17.7; 2048 x 2048 by eight 3.2, by one 7.0.
+  while (a.split < 8 && a.split * 2 <= a.chunks && (int64_t)a.tiles * a.split < 1536) a.split *= 2;
   const DeviceScope scope(m->device);
   if (!scope.ok) return LSTM_INT_E_DEVICE;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);

@@ -12,6 +12,8 @@
 // Bound by memory where it is large and plain: 8192 x 4096 bf16 with a residual 52 us, 4.5 TB/s; by vector instructions with
 // a gate, 36 an element: the same in heads of 128, 71 us, 2.3 TB/s; by the chain load, sum, largest, store where it is small:
 // one row of 2048 5 us.
+#include <algorithm>
+
 #include "lm_common.h"
 
 namespace lstm_int {
@@ -22,6 +24,9 @@ namespace {
 constexpr double kHalf = 0.5 + 0x1p-40;
 
 constexpr int kMostSlots = 4;  // chunks per lane: 2048 columns per wave
+
+// Workgroups along blockIdx.x, blockIdx.y counts on: a dimension of a launch ends at 2^32 threads
+constexpr int kGridBlocks = 1 << 21;
 
 struct NormArgs {
   const void *x, *residual, *gate;
@@ -53,7 +58,8 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % kWaves;
   const bool whole = a.groups == 1;
   const int row_lane = lane & (a.row_lanes - 1);
-  const int64_t row_at = ((int64_t)blockIdx.x * (kBlockWaves / kWaves) + wave / kWaves) * (64 / a.row_lanes) + lane / a.row_lanes;
+  const int64_t rows_at = ((int64_t)blockIdx.y * kGridBlocks + blockIdx.x) * (kBlockWaves / kWaves) + wave / kWaves;
+  const int64_t row_at = rows_at * (64 / a.row_lanes) + lane / a.row_lanes;
   const bool live = row_at < a.rows;
   const int64_t row = live ? row_at : a.rows - 1;  // lanes behind the last row follow it and store nothing
 
@@ -314,7 +320,8 @@ template <class T, int kWaves, int kSlots>
 int launch_norm(const NormArgs &a, hipStream_t s) {
   constexpr int threads = kWaves == 16 ? 1024 : 256;
   const int per_block = threads / 64 / kWaves * (64 / a.row_lanes);
-  const dim3 grid((a.rows + per_block - 1) / per_block);
+  const int64_t blocks = ((int64_t)a.rows + per_block - 1) / per_block;
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, kGridBlocks), (unsigned)((blocks + kGridBlocks - 1) / kGridBlocks));
   return a.gate ? launch(rms_norm_kernel<T, kWaves, kSlots, true>, grid, dim3(threads), s, a)
                 : launch(rms_norm_kernel<T, kWaves, kSlots, false>, grid, dim3(threads), s, a);
 }

@@ -156,3 +156,22 @@ def test_captured_and_on_another_stream():
         assert torch.equal(codes, want[0])
         assert torch.allclose(scales, want[1], rtol=1e-5)  # eps beside a mean square that k changes
         assert np.isfinite(float((codes.float() * scales[:, None]).sum()))
+
+
+# more threads than a dimension of a launch has (2^32), in rows of four waves and of a lane each
+@pytest.mark.parametrize("rows, cols", [((1 << 24) + 5, 1025), ((1 << 29) + 999, 8)])
+def test_more_rows_than_a_grid_dimension_has(rows, cols):
+    x = torch.zeros(rows, cols, dtype=BF16, device="cuda")
+    few, _, _, w = make(64, cols, BF16, seed=12)
+    # behind the workgroups of the first dimension too: 2^21, of one row, and of 256
+    spots = [0, (1 << 21) - 32, (1 << 23) - 32, rows - 64] if cols > 8 else [0, (1 << 29) - 32, rows - 64]
+    for at in spots:
+        x[at:at + 64] = few.cuda()
+    codes, scales = binding.rms_norm_quantize(x, w.cuda())
+    want, want_s = row_codes(reference(few, w)[1])
+    for at in spots:
+        assert (codes[at:at + 64].cpu().double() == want).all()
+        near(scales[at:at + 64], want_s)
+    assert int(torch.count_nonzero(scales)) == 64 * len(spots)
+    del x, codes, scales
+    torch.cuda.empty_cache()

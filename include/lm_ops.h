@@ -131,7 +131,8 @@ int w4_linear_get_quant(const w4_linear_model *model, w4_linear_quant *out);
  * A row that has NaN or an infinity as its scale gives what the formula gives.
  * LSTM_INT_E_INVALID_ARG: NULL, rows < 0, a stride below the row's length with
  * rows > 1, a zero point out of range, an unknown dtype.  LSTM_INT_E_DEVICE: a
- * host-only model.  LSTM_INT_E_UNSUPPORTED: rows beyond 2^24.  rows = 0 is a no-op.
+ * host-only model.  LSTM_INT_E_UNSUPPORTED: rows beyond 2^24, and more than
+ * one launch holds (rows x N beyond some 2^36).  rows = 0 is a no-op.
  */
 int w4_linear_forward(const w4_linear_model *model, const int8_t *x, int64_t x_stride, int64_t rows,
                       const float *row_scales, float scale, int32_t zero_point, void *y,

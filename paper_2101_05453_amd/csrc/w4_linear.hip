@@ -225,8 +225,9 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
 
 // Many rows: a workgroup of eight waves has 128 rows x 128 outputs, a wave 64 x 32 of them.  A chunk's operands and scales
 // go through LDS, two chunks deep.  Needs two chunks or more.  Bound by the latency of a chunk's loads and the stores, with 16
-// waves on a compute unit: 16384 x 640 -> 8192 166 us, 1.0 POP/s (at 192, before the stores went
-// through LDS, it was 150 without them, 177 without the products); 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight needs registers that are not there (two stages: 295 us).
+// waves on a compute unit: 16384 x 640 -> 8192 166 us, 1.0 POP/s (before the stores went through LDS 192, of which 150 without
+// them and 177 without the products); 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight needs registers that are not there
+// (two stages: 295 us).
 template <int kGroup, bool kZero, class T>
 __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   constexpr int per_chunk = kChunk / kGroup;
@@ -367,8 +368,8 @@ int launch_w4(W4Args a, hipStream_t s) {
   // fewer rows to a wave where that takes a workgroup to more of the compute units: 1821 x 6592 -> 64 29 us in 64s, 17 so;
   // 64 x 1024 -> 1024 5.3 and 3.3
   while (!blocks && rows > 16 && (int64_t)a.across * ((a.M + rows - 1) / rows) < 256) rows /= 2;
-  const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536
-  if (count >= (int64_t)1 << 31) return LSTM_INT_E_UNSUPPORTED;
+  const int64_t count = (int64_t)a.across * ((a.M + rows - 1) / rows);  // one dimension: the others end at 65536,
+  if (count > UINT32_MAX / 512) return LSTM_INT_E_UNSUPPORTED;          // and this one at 2^32 threads
   const dim3 grid((unsigned)count), block(512);
   return blocks       ? launch(w4_block_kernel<kGroup, kZero, T>, grid, block, s, a)
          : rows == 16 ? launch(w4_rows_kernel<kGroup, 1, kZero, T>, grid, block, s, a)

@@ -169,3 +169,12 @@ def test_captured_and_on_another_stream(M):
         torch.cuda.synchronize()
         check(y, codes, scales, 128, x2, a)
         assert torch.equal(y, m.forward(xd, ad, dtype=torch.float32))
+
+
+def test_more_than_a_launch_holds_is_refused():
+    codes, scales, x, _, _ = make(64, 8, 1 << 17, 32)
+    m = binding.w4_prepare(codes=codes, scales=scales, group=32)
+    xd, y = torch.from_numpy(x).cuda(), torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda")
+    rc = binding.lm_lib()[0].w4_linear_forward(m._h, xd.data_ptr(), 8, 1 << 24, None, 1.0, 0, y.data_ptr(), 1 << 17, 2, None)
+    torch.cuda.synchronize()
+    assert rc == binding.E_UNSUPPORTED and not y.any()

@@ -893,7 +893,8 @@ def _rms_norm(x, weight, residual, gate, groups, eps, scale, zero_point, codes, 
 def rms_norm(x, weight, residual=None, gate=None, groups=1, eps=1e-6, y=None, new_residual=None):
     """x: CUDA tensor [..., cols] (float32, float16 or bfloat16; rows may be strided); residual, gate, new_residual: of the
     same shape and type; weight: float32 [cols / groups].  Returns y, the norm of x + residual in x's type; new_residual,
-    if given, receives x + residual (it may be residual itself).  Asynchronous on torch's current stream."""
+    if given, receives x + residual (it may be residual itself).  Records no gradients.  Asynchronous on torch's current
+    stream."""
     import torch
 
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if y is None else _dense(y, x.shape, x.dtype, x.device)
@@ -1028,7 +1029,7 @@ def delta_rule(q, k, v, g, beta, state=None, new_state=None, lengths=None, norma
     float32 [T, B, Hv]; any strides but a dense last dimension of q, k, v, y.  state: float32 [B, Hv, Dk, Dv], the state
     before the first step (None: zeros), overwritten with the state after the last one unless new_state takes it.
     lengths: int32 [B]; outputs behind a row's length stay as they are in y (zeros in a y made here).  scale defaults to
-    Dk ** -0.5.  Returns y [T, B, Hv, Dv].  Asynchronous on torch's current stream."""
+    Dk ** -0.5.  Returns y [T, B, Hv, Dv].  Records no gradients.  Asynchronous on torch's current stream."""
     import torch
 
     shape, device = v.shape, v.device

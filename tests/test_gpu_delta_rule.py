@@ -251,6 +251,30 @@ def test_values_that_are_not_finite_stay_in_their_head_and_row():
     check(y, state, want, T, 64 ** -0.5)
 
 
+# many chunks, whose value heads share what is made of a key head
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_heads_that_share_keys_with_lengths_and_values_that_are_not_finite(dtype):
+    T, B, Hk, Hv = 70, 350, 4, 12
+    args = make(T, B, Hk, Hv, 40, 24, dtype, seed=13)
+    lengths = torch.randint(0, T + 1, (B,), generator=torch.Generator().manual_seed(14), dtype=torch.int32)
+    lengths[:6] = torch.tensor([T, 0, 1, 32, 33, 64])
+    want = reference(*args, lengths=lengths)
+    behind = torch.arange(T)[:, None] >= lengths[None]
+    q, k, v, g, beta = (t.clone() for t in args[:5])
+    for t in (q, k, v, g, beta):
+        t[behind] = float("nan")
+    heads = [(0, 1, 20, v), (0, 4, 40, g), (0, 11, 3, beta)]  # of three key heads, beside their neighbours
+    for b, h, at, t in heads:
+        t[at, b, h] = float("nan")
+    y, state = run((q, k, v, g, beta, args[5]), lengths=lengths.cuda())
+    for b, h, at, _ in heads:
+        assert torch.isnan(y[at:, b, h]).all() and torch.isnan(state[b, h]).all()
+        y[:, b, h], state[b, h] = 0, 0
+        want[0][:, b, h], want[1][b, h] = 0, 0
+    assert not y[behind.cuda()].any()
+    check(y, state, want, T, 40 ** -0.5)
+
+
 @pytest.mark.parametrize("T", [1, 96])
 def test_captured_and_on_another_stream(T):
     args = make(T, 2, 1, 2, 128, 64, BF16, seed=12)

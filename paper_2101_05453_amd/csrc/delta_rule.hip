@@ -3,6 +3,7 @@
 //   S <- e^g S;  u = beta (v - S' k);  S <- S + k u';  y = scale S' q
 #include <algorithm>
 
+#include "delta_scale.h"
 #include "lm_common.h"
 
 namespace lstm_int {
@@ -743,14 +744,9 @@ __device__ inline float largest8(f32x4 a, f32x4 b, float m) {
 }
 __device__ inline uint32_t over_column(float m) { return over_column(__float_as_uint(m)); }
 
+// bits of the largest of a column: what the products take as it is
 constexpr uint32_t kLow = 0x41800000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^4, 2^15, infinity
-
-// a power of two that brings numbers whose largest has these bits to 2^10 .. 2^11; with the scale they have already it
-// stays within 2^-120 .. 2^120
-__device__ inline float rescale_of(uint32_t bits, float scale) {
-  const float want = scale_of(bits).up * 0x1p10f;
-  return fminf(fmaxf(want, 0x1p-120f / scale), 0x1p120f / scale);
-}
+__device__ inline bool in_range(uint32_t bits) { return bits - kLow < kHigh - kLow; }
 
 template <class T, int kDk, int kMain, int kCols>
 __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs a) {
@@ -793,10 +789,10 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
 #pragma unroll
       for (int m = 0; m < kTiles; m += 2) top = largest8(st[n][m], st[n][m + 1], top);
       most[n] = over_column(top);
-      // in range, or nothing, or nothing that a scale would help
-      const bool fine = most[n] - kLow < kHigh - kLow || most[n] == 0 || most[n] >= kInf;
+      const bool fine = in_range(most[n]) || most[n] == 0;
       if (__any(!fine)) {
-        const float by = fine ? 1.0f : rescale_of(most[n], up[n]);
+        const int e = exponent_of(__float_as_uint(up[n])), next = fine || most[n] >= kInf ? e : next_exponent(e, most[n], 0);
+        const float by = power_of_two(min(next - e, 126));  // the rest next time
 #pragma unroll
         for (int m = 0; m < kTiles; ++m) st[n][m] *= by;
         up[n] *= by;
@@ -832,6 +828,8 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       for (int e = 0; e < 2; ++e) x[m][e].w = o.x[m][e][lane], p[m][e].w = o.p[m][e][lane];
     const float whole = o.factor[kFwhole][0];
     f32x4 u[kCols][2];
+    Frag added[kCols][2];
+    float keep[kCols];
 #pragma unroll
     for (int n = 0; n < kCols; ++n) {
       const float down = inverse_of_power(up[n]);
@@ -855,6 +853,23 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       mfma_side_by_side<2, 2>(x, part, to);
 #pragma unroll
       for (int m = 0; m < 2; ++m) u[n][m] *= factor(kFx, m) * s.down;
+      // What is added to the state has its scale, or changes it.  The scale is chosen by the largest of what is added and of what is
+      // kept after the decay, and only then applied, to the one, and with the decay in one factor to the other: neither
+      // a scale of a column that has faded nor a decay to all but nothing leads out of the range of a float.
+      {
+        const f32x4 w[2] = {u[n][0] * factor(kFu, 0), u[n][1] * factor(kFu, 1)};
+        const uint32_t wm = over_column(largest8(w[0], w[1], 0.0f)), ws = __float_as_uint(__uint_as_float(wm) * up[n]);
+        const uint32_t kept = __float_as_uint(__uint_as_float(most[n]) * whole);
+        const bool fine = in_range(max(ws, kept)) || (wm | kept) == 0;
+        keep[n] = whole;
+        if (__any(!fine)) {
+          const bool as_it_is = fine || wm >= kInf || kept >= kInf;  // no scale would help
+          const int e = exponent_of(__float_as_uint(up[n])), next = as_it_is ? e : next_exponent(e, kept, wm);
+          keep[n] = as_it_is ? whole : scaled_whole(whole, next - e);
+          up[n] = power_of_two(next);
+        }
+        split8(w[0] * up[n], w[1] * up[n], added[n], minus);
+      }
       // P u
       s = scale_of(over_column(largest8(u[n][0], u[n][1], 0.0f)));
       split8(u[n][0] * s.up, u[n][1] * s.up, part, minus);
@@ -866,24 +881,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         const f32x4 fp = factor(kFp, m) * s.down;
 #pragma unroll
         for (int r = 0; r < 4; ++r) out[n][m][r] = __builtin_fmaf(pu[m][r], fp[r], out[n][m][r]);
-        u[n][m] *= factor(kFu, m) * up[n];
       }
-    }
-    // the state: what is added has the state's scale, or changes it
-    Frag added[kCols][2];
-#pragma unroll
-    for (int n = 0; n < kCols; ++n) {
-      const uint32_t wm = over_column(largest8(u[n][0], u[n][1], 0.0f));
-      const uint32_t kept = __float_as_uint(__uint_as_float(most[n]) * whole), both = max(wm, kept);
-      const bool fine = wm >= kInf || kept >= kInf || wm == 0 || (wm < kHigh && both >= kLow);
-      if (__any(!fine)) {
-        const float by = fine ? 1.0f : rescale_of(both, up[n]);
-#pragma unroll
-        for (int m = 0; m < kTiles; ++m) st[n][m] *= by;
-        u[n][0] *= by, u[n][1] *= by;
-        up[n] *= by;
-      }
-      split8(u[n][0], u[n][1], added[n], minus);
     }
 #pragma unroll
     for (int m = 0; m < kTiles; m += 2) {
@@ -892,7 +890,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       for (int e = 0; e < kP; ++e) f[0][e].w = o.kt[m][e][slot], f[1][e].w = o.kt[m + 1][e][slot];
 #pragma unroll
       for (int n = 0; n < kCols; ++n) {
-        st[n][m] *= whole, st[n][m + 1] *= whole;
+        st[n][m] *= keep[n], st[n][m + 1] *= keep[n];
         f32x4 *to[2] = {&st[n][m], &st[n][m + 1]};
         mfma_side_by_side<kP, 2>(f, added[n], to);
       }

@@ -2,6 +2,7 @@
 // kernels run can be checked exhaustively on a CPU.  Not part of
 // liblstm_int.so.
 #include "calibrate_plan.h"
+#include "delta_scale.h"
 #include "lstm_int_math.h"
 #include "model.h"
 #include "row_stack_plan.h"
@@ -21,6 +22,11 @@ void hm_row_stack_place(int32_t block, int32_t rows, int32_t dirs, int32_t order
   out[0] = p.chain; out[1] = p.dir; out[2] = p.row;
   out[3] = row_stack_link(order, p.dir, dirs);
 }
+
+// scales of the delta rule's state: e becomes the result; kept and keep at the new scale
+int32_t hm_delta_next_exponent(int32_t e, uint32_t kept, uint32_t added) { return next_exponent(e, kept, added); }
+float hm_delta_scaled_whole(float whole, int32_t d) { return scaled_whole(whole, d); }
+float hm_power_of_two(int32_t e) { return power_of_two(e); }
 
 // layer norm of one row through ln_row / ln_apply
 void hm_layernorm(const int16_t *q, int32_t n, const int16_t *qL, const int32_t *qb, int32_t M,

@@ -145,9 +145,14 @@ void w4_linear_destroy(w4_linear_model *model);
  * (' is the transpose; g the log of the decay, beta the rate of writing).  Key
  * head h serves the value heads h * value_heads / key_heads and the ones behind
  * it.  normalize = 1: k and q are first divided by sqrt(sum of squares + 1e-6).
- * Sums and the state are float32; calls of 12 steps and more run 32 steps at a
- * time on the matrix cores, with float32 operands in two scaled parts of fp16,
- * 22 bits, so that results are as exact as float32 products.
+ * Sums and the state are float32.  Calls of 12 steps and more run 32 steps at a
+ * time on the matrix cores, with float32 operands in two scaled parts of fp16:
+ * 22 bits of each element, and of one far below the largest 2^-39 of that
+ * largest, of a column of the state 2^-30 and of a key 2^-27.  The largest is
+ * over a key or query, over a state's column (one value column, all key
+ * columns) and, for the values, over a column's 32 steps, so that a value 2^17
+ * times as large as its neighbours costs their outputs bits, those of earlier
+ * steps among them.  Shorter calls run step by step in float32.
  *   q, k    DEVICE dtype [T, B, key_heads, key_dim]
  *   v, y    DEVICE dtype [T, B, value_heads, value_dim]
  *   g, beta DEVICE float32 [T, B, value_heads]

@@ -157,10 +157,18 @@ int launch_step(const DeltaArgs &a, hipStream_t s) {
 //
 // Products run on the fp16 MFMA, whose products are exact and whose sums are float32.  A float32 operand is scaled by a power
 // of two -- each row of a left operand and each column of a right one by its own -- and taken as two fp16 parts: 22 bits of
-// each element, and 2^-25 of the largest.  Of the products of parts the one of the two low ones, 2^-22 of the others, is
-// left out.  bf16 and fp16 keys and queries are one part.  So results are as exact as float32 products, at two or three
-// MFMAs for one, where the float32 MFMA takes 16 times the time.  (Three bf16 parts, which need no scales, took three to six,
-// and more vector instructions: 777 ragged steps of 5 x 6 float32 heads 141 us, 96 so.)
+// each element, down to a floor of 2^-25, where the largest is just below 2^15 (kTop, delta_scale.h; a column of the state
+// 2^5 .. 2^15, keys 2^2 .. 2^3).  Of the products of parts the one of the two low ones, 2^-22 of the others, is left out.  bf16
+// and fp16 keys and queries are one part.  Two or three MFMAs for one product, where the float32 MFMA takes 16 times the time.
+// (Three bf16 parts, 24 bits, which need no scales, took three to six, and more vector instructions: 777 ragged steps of 5 x 6
+// float32 heads 141 us, 96 so.)
+//
+// So a sum is as near as one of float32 products relative to the row and the column that it is made of, not to each of their
+// elements: one far below its row's or column's largest is known to 2^-39 of that largest, in a key to 2^-27, in the state to
+// 2^-30 (2^-36 where its scale is new).  A right-hand side's column has the 32 steps of a chunk, so that a value 2^17 times as
+// large as the others costs these the first of their bits, earlier steps too, and a value 2^39 times as large all of them; a
+// column of the state has all key rows.  (With all largest at 1 .. 2, a value 10^6 times as large left 5 bits of the steps
+// before it.)
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kChunk = 32;
 constexpr int kHeadsOfGrid = 1 << 15;  // blockIdx.y of the first kernel, blockIdx.z counts on
@@ -187,14 +195,6 @@ union Frag {
 
 __device__ inline f32x4 mfma(const Frag &a, const Frag &b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0); }
 
-// scale and 1 / scale, powers of two, that bring numbers whose largest has these bits (without sign) to 1 .. 2
-struct Scale {
-  float up, down;
-};
-__device__ inline Scale scale_of(uint32_t bits) {
-  bits = min(max(bits & 0x7f800000u, 0x00800000u), 0x7e800000u);
-  return {__uint_as_float(0x7f000000u - bits), __uint_as_float(bits)};
-}
 __device__ inline uint32_t bits_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 // the largest over the four lanes of a column
 __device__ inline uint32_t over_column(uint32_t v) {
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
     sk[m] += __shfl_xor(sk[m], 32);
     sq[m] += __shfl_xor(sq[m], 16);
     sq[m] += __shfl_xor(sq[m], 32);
-    const Scale ks = scale_of(over_column(mk[m])), qs = scale_of(over_column(mq[m]));
+    const Scale ks = scale_of<kKeyTop>(over_column(mk[m])), qs = scale_of<kTop>(over_column(mq[m]));
     inv_sk[m] = ks.down, inv_sq[m] = qs.down;
     if (g == 0) {
       norm_k[16 * m + i] = d.normalize ? 1.0f / sqrtf(sk[m] + kNormEps) : 1.0f;
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) most = max(most, bits_of(v[e][j]));
         }
-        const Scale s = scale_of(over_column(most));  // lanes i, i + 16, ...: the row's
+        const Scale s = scale_of<kTop>(over_column(most));  // lanes i, i + 16, ...: the row's
         Frag f[2];
         split8(v[0] * s.up, v[1] * s.up, f, minus_one());
 #pragma unroll
@@ -745,7 +745,7 @@ __device__ inline float largest8(f32x4 a, f32x4 b, float m) {
 __device__ inline uint32_t over_column(float m) { return over_column(__float_as_uint(m)); }
 
 // bits of the largest of a column: what the products take as it is
-constexpr uint32_t kLow = 0x41800000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^4, 2^15, infinity
+constexpr uint32_t kLow = 0x42000000u, kHigh = 0x47000000u, kInf = 0x7f800000u;  // 2^5, 2^15, infinity
 __device__ inline bool in_range(uint32_t bits) { return bits - kLow < kHigh - kLow; }
 
 template <class T, int kDk, int kMain, int kCols>
@@ -762,7 +762,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
   const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, slot = slot_of(i, g);
   const float minus = minus_one();
   int col[kCols];
-  f32x4 st[kCols][kTiles];  // the state times its column's scale, which changes where the column leaves 2^4 .. 2^15
+  f32x4 st[kCols][kTiles];  // the state times its column's scale, which changes where the column leaves 2^5 .. 2^15
   float up[kCols];
   const int64_t head = (int64_t)bh * d.Dk * d.Dv;
 #pragma unroll
@@ -846,7 +846,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         }
       }
       // u
-      Scale s = scale_of(over_column(largest8(rhs[n][0], rhs[n][1], 0.0f)));
+      Scale s = scale_of<kTop>(over_column(largest8(rhs[n][0], rhs[n][1], 0.0f)));
       split8(rhs[n][0] * s.up, rhs[n][1] * s.up, part, minus);
       u[n][0] = u[n][1] = f32x4{0, 0, 0, 0};
       f32x4 *to[2] = {&u[n][0], &u[n][1]};
@@ -858,7 +858,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
       // a scale of a column that has faded nor a decay to all but nothing leads out of the range of a float.
       {
         const f32x4 w[2] = {u[n][0] * factor(kFu, 0), u[n][1] * factor(kFu, 1)};
-        const uint32_t wm = over_column(largest8(w[0], w[1], 0.0f)), ws = __float_as_uint(__uint_as_float(wm) * up[n]);
+        const uint32_t wm = over_column(largest8(w[0], w[1], 0.0f)), ws = __float_as_uint(__uint_as_float(wm) * (up[n] * (1 << kKeyTop)));
         const uint32_t kept = __float_as_uint(__uint_as_float(most[n]) * whole);
         const bool fine = in_range(max(ws, kept)) || (wm | kept) == 0;
         keep[n] = whole;
@@ -871,7 +871,7 @@ __global__ __launch_bounds__((kMain + 4) * 64) void delta_scan_kernel(ChunkArgs 
         split8(w[0] * up[n], w[1] * up[n], added[n], minus);
       }
       // P u
-      s = scale_of(over_column(largest8(u[n][0], u[n][1], 0.0f)));
+      s = scale_of<kTop>(over_column(largest8(u[n][0], u[n][1], 0.0f)));
       split8(u[n][0] * s.up, u[n][1] * s.up, part, minus);
       f32x4 pu[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
       f32x4 *to2[2] = {&pu[0], &pu[1]};

@@ -27,6 +27,11 @@ void hm_row_stack_place(int32_t block, int32_t rows, int32_t dirs, int32_t order
 int32_t hm_delta_next_exponent(int32_t e, uint32_t kept, uint32_t added) { return next_exponent(e, kept, added); }
 float hm_delta_scaled_whole(float whole, int32_t d) { return scaled_whole(whole, d); }
 float hm_power_of_two(int32_t e) { return power_of_two(e); }
+// of an operand (keys != 0: of keys): scale and 1 / scale
+void hm_delta_scale(uint32_t bits, int keys, float out[2]) {
+  const Scale s = keys ? scale_of<kKeyTop>(bits) : scale_of<kTop>(bits);
+  out[0] = s.up, out[1] = s.down;
+}
 
 // layer norm of one row through ln_row / ln_apply
 void hm_layernorm(const int16_t *q, int32_t n, const int16_t *qL, const int32_t *qb, int32_t M,

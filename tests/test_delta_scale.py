@@ -9,7 +9,7 @@ import pytest
 
 from paper_2101_05453_amd import build as libbuild
 
-UP = 120
+UP, TOP, KEYS = 120, 11, 2  # the state is brought to 2^11 .. 2^12; what is added comes times keys of 2^2 and more
 
 
 @pytest.fixture(scope="module")
@@ -36,11 +36,11 @@ def check(hm, e, kept, added):
     assert -UP <= n <= UP
     if kept or added:
         # the larger one in the column's scale, then in the new one; where the scale is at its end it is on that side
-        most = max(value(kept), math.ldexp(value(added), e))
+        most = max(value(kept), math.ldexp(value(added), e + KEYS))
         new = math.ldexp(most, n - e)
         normal = value(kept) >= 2.0 ** -126 and added == 0 or value(added) >= 2.0 ** -126 and kept == 0
-        assert new < 2 ** 11 or n == -UP
-        assert new >= 2 ** 10 or n == UP or not normal
+        assert new < 2 ** (TOP + 1) or n == -UP
+        assert new >= 2 ** TOP or n == UP or not normal
     return n
 
 
@@ -50,7 +50,7 @@ def test_every_scale_of_one_number(hm):
             n = check(hm, e, b, 0)
             by = hm.hm_power_of_two(min(n - e, 126))  # what a column is brought by before a chunk
             # at n = -UP the scale can only have come down or stayed, and a float times that is a float
-            assert by > 0 and (by <= 1 if n == -UP else np.float32(value(b)) * np.float32(by) < 2 ** 11)
+            assert by > 0 and (by <= 1 if n == -UP else np.float32(value(b)) * np.float32(by) < 2 ** (TOP + 1))
             check(hm, e, 0, b)
 
 
@@ -78,5 +78,17 @@ def test_what_is_kept_at_the_new_scale_is_a_float(hm):
                     n = check(hm, e, int(kept.view(np.uint32)), int(a.view(np.uint32)))
                     keep = np.float32(hm.hm_delta_scaled_whole(w, n - e))
                     # at n = -UP what is kept is m times a decay and no more than one
-                    assert 0 <= m * keep < (2 ** 15 + 1 if n == -UP else 2 ** 12)
-                    assert a * np.float32(hm.hm_power_of_two(n)) < 2 ** 11
+                    assert 0 <= m * keep < (2 ** 15 + 1 if n == -UP else 2 ** (TOP + 2))
+                    assert a * np.float32(hm.hm_power_of_two(n)) < 2 ** (TOP + 1 - KEYS)
+
+
+@pytest.mark.parametrize("keys, top", [(0, 14), (1, 2)])
+def test_scales_of_operands(hm, keys, top):
+    out = (C.c_float * 2)()
+    for b in BITS + [0x7f800000, 0x7fc00000]:  # infinity and NaN too
+        hm.hm_delta_scale(b, keys, out)
+        up, down = out
+        assert up * down == 1 and math.frexp(up)[0] == 0.5 and 2.0 ** -126 <= min(up, down)
+        x = np.float32(value(b)) * np.float32(up)
+        if value(b) < 2.0 ** 128:  # not infinity, not NaN: fp16 holds it, and it is where it should be
+            assert x < 2 ** (top + 1) <= 2 ** 15 and (x >= 2 ** top or value(b) < 2.0 ** (top - 126))

@@ -40,7 +40,7 @@ def reference(q, k, v, g, beta, S):
     return y, S, sizes
 
 
-HELD = 2.0 ** -25  # of the largest of a column and chunk: what two parts of fp16 leave of any of its numbers
+HELD = 2.0 ** -39  # of the largest of a column and chunk: what two parts of fp16 leave of any of its numbers
 
 
 def check(args, y, state, scale_q):
@@ -133,3 +133,66 @@ def test_a_cleared_state_and_small_values(size, dtype):
     args[2] *= 1e-20
     args[3][32] = float("-inf")
     run_and_check(args)
+
+
+# A value far louder than the others, at the last step of a chunk: the outputs before it are of the size they have without it.
+# Per column: the roundings of check(), and 2^-39 of the chunk's largest value, at two places (the right-hand side, u) and in
+# a sum over 32 steps of products of unit vectors.
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("loud", [1e3, 1e5, 1e7])
+@pytest.mark.parametrize("B, Hk, Hv, Dk, Dv", SIZES)
+def test_a_loud_step_leaves_the_steps_before_it(B, Hk, Hv, Dk, Dv, loud, dtype):
+    T = 64
+    args = make(T, B, Hk, Hv, Dk, Dv, dtype, seed=Dk + 2)
+    want = reference(*args)[0]
+    args[2][63] *= loud
+    d = [t.cuda() for t in args]
+    y = binding.delta_rule(*d[:5], state=d[5], normalize=True).double().cpu().numpy()[:63]
+    quiet = [t[:63] for t in args[:5]] + [args[5]]
+    sizes = reference(*quiet)[2]
+    walk = 4 * math.sqrt(T + 1) * (8 + math.sqrt(Dk)) * 2.0 ** -24 * sizes[..., None]
+    largest = np.abs(args[2].double().numpy()).max(0)
+    off = np.abs(y - want[:63]) - np.abs(want[:63]) * torch.finfo(dtype).eps / 2
+    bound = (walk + 64 * 2.0 ** -39 * largest) * Dk ** -0.5
+    assert (off <= bound).all(), (off / bound).max()
+    assert loud > 1e5 or (off <= 1e-3 * np.sqrt((want[:63] ** 2).mean())).all()
+
+
+# A value far louder than the others, forgotten within its chunk: what comes behind it is of its own size.  Per column, as above:
+# what is off is 2^-39 of the loud value, not of what is left of it.
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("loud", [1e3, 1e5, 1e7])
+@pytest.mark.parametrize("at", [5, 30])
+def test_a_loud_value_is_forgotten(at, loud, dtype):
+    args = make(64, 1, 1, 2, 64, 48, dtype, seed=8)
+    args[2][at] *= loud
+    args[3][at + 1] = -math.log(loud) - 6
+    run_and_check(args)
+
+
+# Float32 outputs, step by step: a sum of Dk or 32 products, each off by 2^-22 of itself and independent of the others, is off by
+# 2^-22 of the root of the sum of their squares: for a query of normal draws |S| / sqrt(Dk), with |S| the root of the squares
+# of the first state and all writes, decayed.  A chunk's seven products add theirs to the state, and chunks add up like a
+# random walk.  16 for the seven products, for sums in float32 and for the largest of many draws; leaving out one low part of
+# any operand is 500 and more.
+@pytest.mark.parametrize("T, B, Hk, Hv, Dk, Dv", [(16, 1, 1, 1, 128, 128), (33, 2, 1, 2, 100, 50), (64, 1, 1, 1, 128, 128), (130, 1, 1, 2, 256, 64),
+                                                  (200, 3, 2, 2, 128, 128), (257, 1, 1, 1, 200, 256), (300, 1, 3, 6, 16, 48), (500, 1, 1, 1, 7, 5),
+                                                  (70, 70, 2, 4, 128, 100)])
+def test_every_output_has_the_bits_of_float32(T, B, Hk, Hv, Dk, Dv):
+    args = make(T, B, Hk, Hv, Dk, Dv, FP32, seed=T)
+    want, want_S, _ = reference(*args)
+    d = [t.cuda() for t in args]
+    y = binding.delta_rule(*d[:5], state=d[5], normalize=True).double().cpu().numpy()
+    k, v, g, beta, S = (t.double().numpy() for t in args[1:])
+    k = np.repeat(k / np.sqrt((k * k).sum(3, keepdims=True) + 1e-6), Hv // Hk, 2)
+    n2 = (S * S).sum((2, 3))
+    for t in range(T):
+        S = S * np.exp(g[t])[:, :, None, None]
+        Sk = (S * k[t][..., None]).sum(2)
+        n2 = n2 * np.exp(2 * g[t]) + beta[t] ** 2 * ((v[t] ** 2).sum(2) + (Sk ** 2).sum(2))
+        S = S + k[t][..., None] * (beta[t][..., None] * (v[t] - Sk))[:, :, None]
+        bound = 16 * 2.0 ** -22 * np.sqrt(n2 / Dk * (1 + t / 32)) * Dk ** -0.5
+        off = np.sqrt(((y[t] - want[t]) ** 2).sum(2))
+        assert (off <= bound).all(), (t, (off / bound).max())
+    off = np.sqrt(((d[5].double().cpu().numpy() - want_S) ** 2).sum((2, 3)))
+    assert (off <= 16 * 2.0 ** -22 * np.sqrt(n2 * (1 + T / 32))).all()

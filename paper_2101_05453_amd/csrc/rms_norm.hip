@@ -171,8 +171,10 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
   }
 
   if (a.codes) {
-    // n in float32, at most ten roundings off
-    float n[kSlots][8];
+    // n in float32, at most ten roundings off where no product on the way leaves float32's normal range.  One that does is
+    // below 2^-126, so what becomes of it is below 2^-94 and next to nothing (in_float, usable), unless its weight or gate is
+    // beyond 2^16: `far` is the largest of them.
+    float n[kSlots][8], far = 0;
     uint32_t largest = 0;  // bits of the largest |n|; of a NaN, if there is one
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
@@ -185,8 +187,10 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
         float v = (float)rx[s].e[i];
         if (res) v += (float)rr[s].e[i];
         v = v * iv * wt.e[i];
+        far = __builtin_fmaxf(far, fabsf(wt.e[i]));
         if constexpr (kGate) {
           const float z = (float)rg[s].e[i];
+          far = __builtin_fmaxf(far, fabsf(z));
           // e^-z = 2^(t + lo), t the rounded product
           constexpr float kLog2e = -1.44269504f, kLow = -1.92596299e-8f, kLn2 = 0.693147181f;
           const float t = z * kLog2e, lo = __builtin_fmaf(z, kLow, __builtin_fmaf(z, kLog2e, -t));
@@ -198,6 +202,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
       }
     }
 
+    if (far > 0x1p16f) largest = 0x7f800000u;
     // v = n / s + 1/2 decides its floor where it is further from a border than ten roundings of it
     auto decided = [](float v) { return fabsf(v - floorf(v) - 0.5f) < __builtin_fmaf(fabsf(v), -0x1p-20f, 0.5f - 0x1p-20f); };
     static_assert(kSlots * 8 <= 32, "a bit for each element of a lane");
@@ -218,7 +223,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
     uint32_t open = 0;  // elements whose code float32 does not decide
     if (a.scale != 0) {
       const float mul = (float)(1.0 / a.scale);
-      const bool usable = mul >= 0x1p-80f && mul <= 0x1p80f;
+      const bool usable = mul >= 0x1p-80f && mul <= 0x1p80f && largest < 0x7f800000u;
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) {
         if (at[s].count <= 0) continue;
@@ -249,7 +254,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(Nor
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) row_largest = max(row_largest, (uint32_t)part[1][wave - w + i]);
       }
-      // a NaN, or numbers that float32 may not hold to all their bits: the whole row in double precision
+      // a NaN, or numbers that float32 may not hold to all their bits or that come of such: the whole row in double precision
       const float top = __uint_as_float(row_largest);
       const bool in_float = top >= 0x1p-80f && top <= 0x1p80f;
       const float from = in_float ? top * (1 - 0x1p-18f) : -1.0f;  // what may be the largest

@@ -51,8 +51,9 @@ __device__ inline double shfl_xor_d(double v, int mask) {
   return b.d;
 }
 
+// With a gate, five waves to a SIMD: float32, 4096 x 2048, 24.9 us; 26.4 at four, which the compiler takes by itself
 template <class T, int kWaves, int kSlots, bool kGate>
-__global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void rms_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(kWaves == 16 ? 1024 : 256, kWaves != 16 && kSlots == 1 && kGate ? 5 : 1) void rms_norm_kernel(NormArgs a) {
   constexpr int kBlockWaves = kWaves == 16 ? 16 : 4;
   __shared__ double part[3][kBlockWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % kWaves;

@@ -192,11 +192,11 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256, kWaves != 16 && kSlots =
         if constexpr (kGate) {
           const float z = (float)rg[s].e[i];
           far = __builtin_fmaxf(far, fabsf(z));
-          // e^-z = 2^(t + lo), t the rounded product
+          // e^-z = 2^(t + lo), t the rounded product; from 2^128 on infinity as it is, and the factor zero (lo times it is NaN)
           constexpr float kLog2e = -1.44269504f, kLow = -1.92596299e-8f, kLn2 = 0.693147181f;
           const float t = z * kLog2e, lo = __builtin_fmaf(z, kLow, __builtin_fmaf(z, kLog2e, -t));
           const float e = __builtin_amdgcn_exp2f(t);
-          v *= z * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, fabsf(t) < 128.0f ? lo * kLn2 : 0.0f, e));
+          v *= z * __builtin_amdgcn_rcpf(1.0f + (fabsf(t) < 128.0f ? __builtin_fmaf(e, lo * kLn2, e) : e));
         }
         n[s][i] = v;
         largest = max(largest, __float_as_uint(v) & 0x7fffffffu);

@@ -172,7 +172,9 @@ void w4_linear_destroy(w4_linear_model *model);
  * the steps before it within the same 32; nothing reaches another row or head.
  * T = 0 copies the state; B = 0 is a no-op.
  * LSTM_INT_E_INVALID_ARG: NULL, a negative extent, value_heads no multiple of
- * key_heads, an unknown dtype, a normalize other than 0 and 1.  LSTM_INT_E_BAD_RANGE: a scale that is not finite.
+ * key_heads, an unknown dtype, a normalize other than 0 and 1, a stride of y
+ * below value_dim (either way) in a dimension of more than one.
+ * LSTM_INT_E_BAD_RANGE: a scale that is not finite.
  * LSTM_INT_E_UNSUPPORTED: key_dim or value_dim beyond 256; B * value_heads
  * beyond 2^20; T beyond 2^24.  LSTM_INT_E_WORKSPACE.
  */

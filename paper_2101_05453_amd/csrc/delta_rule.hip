@@ -1004,6 +1004,9 @@ int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, 
   if (p->steps > 0 && (!q || !k || !v || !g || !beta || !y)) return LSTM_INT_E_INVALID_ARG;
   const size_t need = delta_rule_workspace_bytes(p);
   if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255))) return LSTM_INT_E_WORKSPACE;
+  const int64_t extents[3] = {p->steps, p->batch, p->value_heads};
+  for (int i = 0; i < 3; ++i)  // y: neighbours would be in each other's place
+    if (p->steps && extents[i] > 1 && p->y_stride[i] < p->value_dim && p->y_stride[i] > -p->value_dim) return LSTM_INT_E_INVALID_ARG;
   DeltaArgs a{};
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.lengths = lengths; a.state = state; a.new_state = new_state; a.y = y;
   for (int i = 0; i < 3; ++i) {

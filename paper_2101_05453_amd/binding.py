@@ -906,10 +906,10 @@ def rms_norm(x, weight, residual=None, gate=None, groups=1, eps=1e-6, y=None, ne
 def rms_norm_quantize(x, weight, residual=None, gate=None, groups=1, eps=1e-6, scale=None, zero_point=0, codes=None,
                       scales=None, y=None, new_residual=None):
     """As rms_norm, into int8 codes: returns (codes [..., cols], scales float32 [...]), a scale of each row; or (codes, None)
-    with a fixed scale and zero point, such as a model's (s_x, zp_x).  y, if given, also receives the norm in x's type."""
+    with a fixed scale and a zero point (which codes with a scale of each row do not have), such as a model's (s_x, zp_x).  y, if given, also receives the norm in x's type."""
     import torch
 
-    assert scale is None or scale > 0
+    assert zero_point == 0 if scale is None else scale > 0
     codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else _dense(codes, x.shape, torch.int8, x.device)
     if scale is not None:
         scales = None

@@ -66,3 +66,11 @@ def test_gates_that_are_closed(groups, dtype):
         gate[:, 10 + 100 * i] = z
     gate[4] = -1e4  # a row of nothing but closed gates: codes 0
     check(x.to(dtype), torch.rand(1024 // groups, generator=g) + 0.5, gate=gate.to(dtype), groups=groups)
+
+
+def test_a_zero_point_without_a_scale_is_refused():
+    x, w = torch.ones(2, 64, dtype=BF16, device="cuda"), torch.ones(64, device="cuda")
+    with pytest.raises(AssertionError):
+        binding.rms_norm_quantize(x, w, zero_point=5)
+    codes, _ = binding.rms_norm_quantize(x, w, scale=1.0, zero_point=5)
+    assert (codes == 6).all()

@@ -152,14 +152,17 @@ void w4_linear_destroy(w4_linear_model *model);
  * over a key or query, over a state's column (one value column, all key
  * columns) and, for the values, over a column's 32 steps, so that a value 2^17
  * times as large as its neighbours costs their outputs bits, those of earlier
- * steps among them.  Shorter calls run step by step in float32.
+ * steps among them.  Shorter calls run step by step in float32.  What overflows
+ * float32 gives infinities and NaN: sums of squares of k and q, with normalize
+ * too (elements beyond 2^60), S' k and S' q before the decay, and results.
  *   q, k    DEVICE dtype [T, B, key_heads, key_dim]
  *   v, y    DEVICE dtype [T, B, value_heads, value_dim]
  *   g, beta DEVICE float32 [T, B, value_heads]
  *           each with strides, in elements, of step, batch row and head, that
  *           may be anything for the inputs (a slice of a projection's output);
  *           the last dimension of q, k, v, y is dense.
- *           g = -infinity clears the state (of finite numbers).
+ *           g = -infinity clears the state (of finite numbers); a sum of g over
+ *           32 steps stays below 80 (a decay has none above 0).
  *   lengths DEVICE int32 [B]: row b has min(max(lengths[b], 0), T) steps; inputs
  *           behind them are not used and outputs there left as they are;
  *           NULL: every row has T

@@ -324,7 +324,8 @@ struct Inputs {
 };
 
 // One wave per chunk and value head, or all of a key head's: X, P and the factors of its steps.  Vector instructions and
-// the chain of the substitution bound it: 64 chunks of 8 x 16 key heads of 128, two value heads each, 87 us.
+// the chain of the substitution bound it: 64 chunks of 8 x 16 key heads of 128, two value heads each, 84 us, 39 %
+// of whose cycles issue vector instructions.
 template <class T, int kDk, bool kWhole>  // kWhole: key_dim = kDk
 __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
   constexpr int kLd = 36, kBlocks = kDk / 32;
@@ -536,9 +537,9 @@ __global__ __launch_bounds__(64) void delta_prep_kernel(ChunkArgs a) {
 // in the MFMA's order, with the chunk after it already requested.  kBuffers = 1 where two do not fit.
 //
 // With a workgroup on each compute unit it is bound by the issue of vector instructions: 1060 to a SIMD and chunk (parts of
-// the state and their scales, the loaders' transposition), 51 % of all cycles, 68 % with the others; LDS 24 %, MFMA 23 %.
-// 2048 steps of 8 x 32 heads of 128 x 128: 250 us, 3.9 us a chunk.  With fewer it is bound by the chain of a chunk, K S ->
-// u -> S: 1.6 us for 32 steps.
+// the state and their scales, the loaders' transposition), 53 % of all cycles, 67 % with the others; LDS 18 %, MFMA 24 %.
+// 2048 steps of 8 x 32 heads of 128 x 128: 221 us, 3.5 us a chunk.  With fewer it is bound by the chain of a chunk, K S ->
+// u -> S: 1.5 us for 32 steps, for which the scale of what is added to the state comes in front of P u (1.6 behind it).
 template <class T, int kDk, int kMain, int kCols>
 struct Scan {
   static constexpr int kP = kParts<T>, kBlocks = kDk / 32, kLoaders = 4, kColumns = 16 * kMain * kCols;
@@ -938,8 +939,8 @@ int launch_scan(const ChunkArgs &a, hipStream_t s) {
 }
 
 // As many columns to a workgroup as leave one for each compute unit: their operands come from memory once.  (2048 steps of
-// 8 x 32 heads, 128 columns in four waves of 32, in eight waves of 16, 64 columns in four of 16: 373, 382, 443 us; float32
-// 511, 612, 627.)
+// 8 x 32 heads, 128 columns in four waves of 32, 64 columns in four of 16: 335 and 396 us; float32 426 and 532.  Eight waves
+// of 16 were between the two.)
 template <class T, int kDk>
 int launch_scan(const ChunkArgs &a, hipStream_t s) {
   const int64_t heads = (int64_t)a.d.B * a.d.Hv;
@@ -969,8 +970,8 @@ int launch_chunks(const ChunkArgs &a, hipStream_t s) {
   return a.d.Dk <= 64 ? launch_chunks<T, 64>(a, s) : a.d.Dk <= 128 ? launch_chunks<T, 128>(a, s) : launch_chunks<T, 256>(a, s);
 }
 
-// A chunk takes the time of some twelve steps: 16 heads of 128 x 128, 8, 12 and 16 steps: 18, 24 and 31 us step by step, 20,
-// 22 and 21 in one chunk; with 64 rows 74, 97 and 121, and 91, 93 and 93.  The loads of a chunk take four columns at once.
+// A chunk takes the time of some twelve steps of few heads, sixteen of many: 16 heads of 128 x 128, 8, 12 and 16 steps: 17, 23
+// and 29 us step by step, 20, 20 and 21 in one chunk; with 64 rows 57, 74 and 90, and 92, 93 and 93.  The loads of a chunk take four columns at once.
 bool in_chunks(const delta_rule_args *p) { return p->steps >= 12 && p->key_dim >= 4 && p->value_dim >= 4; }
 
 int check(const delta_rule_args *p) {
@@ -1021,8 +1022,8 @@ int delta_rule_forward(int32_t device, const delta_rule_args *p, const void *q, 
   if (in_chunks(p)) {
     ChunkArgs c{a, static_cast<uint32_t *>(workspace), (p->steps + kChunk - 1) / kChunk, 1};
     // The products of keys and queries are the same for all value heads of a key head: a wave for all of them, as long as
-    // that leaves the device full.  2048 steps, two value heads to each of 8 x 16 key heads 379 us instead of 400, of 4 x 16
-    // 183 instead of 191; four to each of 8 x 8 311 instead of 342.
+    // that leaves the device full.  2048 steps, two value heads to each of 8 x 16 key heads 335 us instead of 348, of 4 x 16
+    // 176 instead of 182; four to each of 8 x 8 292 instead of 308.
     if ((int64_t)p->batch * p->key_heads * c.chunks >= 4096) c.heads = p->value_heads / p->key_heads;
     return p->dtype == LM_F32 ? launch_chunks<float>(c, s) : p->dtype == LM_F16 ? launch_chunks<_Float16>(c, s) : launch_chunks<__bf16>(c, s);
   }

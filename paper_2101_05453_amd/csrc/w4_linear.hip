@@ -226,8 +226,9 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
 // Many rows: a workgroup of eight waves has 128 rows x 128 outputs, a wave 64 x 32 of them.  A chunk's operands and scales
 // go through LDS, two chunks deep.  Needs two chunks or more.  Bound by the latency of a chunk's loads and the stores, with 16
 // waves on a compute unit: 16384 x 640 -> 8192 166 us, 1.0 POP/s (before the stores went through LDS 192, of which 150 without
-// them and 177 without the products); 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight needs registers that are not there
-// (two stages: 295 us).
+// them and 177 without the products); 4096 x 4096 -> 4096 105 us, 1.3 POP/s.  More in flight by way of registers needs
+// more than there are (two stages: 295 us); loads straight into LDS were not tried.  The first product in groups of 32: 253 us,
+// and 446 with a zero point, where 21 registers are spilled.
 template <int kGroup, bool kZero, class T>
 __global__ __launch_bounds__(512, 4) void w4_block_kernel(W4Args a) {
   constexpr int per_chunk = kChunk / kGroup;

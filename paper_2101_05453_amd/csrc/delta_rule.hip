@@ -971,7 +971,8 @@ int launch_chunks(const ChunkArgs &a, hipStream_t s) {
 }
 
 // A chunk takes the time of some twelve steps of few heads, sixteen of many: 16 heads of 128 x 128, 8, 12 and 16 steps: 17, 23
-// and 29 us step by step, 20, 20 and 21 in one chunk; with 64 rows 57, 74 and 90, and 92, 93 and 93.  The loads of a chunk take four columns at once.
+// and 29 us step by step, 20, 20 and 21 in one chunk; with 64 rows 57, 74 and 90, and 92, 93 and 93.  The loads of a chunk take
+// four columns at once.
 bool in_chunks(const delta_rule_args *p) { return p->steps >= 12 && p->key_dim >= 4 && p->value_dim >= 4; }
 
 int check(const delta_rule_args *p) {
